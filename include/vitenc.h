@@ -296,6 +296,117 @@ vit_status_t vit_preprocess_tiles(const uint8_t* image, int32_t height, int32_t 
                                   size_t out_capacity_bytes, void* stream);
 
 /*
+ * The paged key/value cache of the instance that pulls the tokens (paper Sec. 2: decoder-only back ends take image
+ * tokens as a part of the prompt, cross-attention back ends let text attend to them; either way they become keys and
+ * values of a layer).  A layer's cache is two pools of n_pages pages, [n_pages, kv_heads, page_size, head_dim] each, bf16
+ * or fp32; a request's row of the block table names its pages in order, so that its token `at` lies in
+ * page table[at / page_size] at place at % page_size: slot number page * page_size + at % page_size.
+ * page_size is a power of two, 8 to 4096; n_pages * page_size is below 2^31.  All pointers in the three structs are DEVICE
+ * pointers; the calls are asynchronous on `stream`, run on the calling thread's current device, where all buffers
+ * must live, allocate nothing, keep nothing from one call for the next and may be captured into a graph.
+ *
+ * vit_pages_plan: where a step's new tokens go.  Of request r, cached_lens[r] tokens are in the cache and new_lens[r] come
+ * (both 0 to 2^30; what is negative counts as 0); the step's tokens are packed in request order into n_rows rows.
+ *   query_offsets [n_requests + 1]  first row of each request, and the end of the last one.  Tokens past n_rows are left
+ *                                   out: the offsets stop at n_rows.
+ *   kv_lens [n_requests]            tokens in the cache once the step's are (may be cached_lens itself).
+ *   slots [n_rows]                  slot of each row's token; -1 for rows behind the last request's.
+ *   page_offsets [n_requests + 1]   first entry of free_pages that the request takes: entries *taken and on are free.
+ *                                   Its tokens fill its last page first.  The pages it takes are entered into its row of
+ *                                   the block table; nothing else of the table is written.
+ *   counts [2]                      entries of free_pages that are taken now (counts may be `taken` itself, for a step
+ *                                   that a graph repeats), and the number of new tokens that got no slot.
+ * A token whose page would lie past table_width, past the end of free_pages or outside 0 ... n_pages - 1 gets slot -1 (the
+ * entry, if there is one for it, becomes -1).  `taken` may be NULL: 0.
+ * Outputs overlap neither inputs nor each other, but for the two named.
+ *
+ * vit_pages_append: rows i of k and v (head h's values at i * stride + h * head_dim) to slots[i] of the pools.  Rows with a slot
+ * outside 0 ... n_pages * page_size - 1 are passed over.  No slot may be given twice.  Pointers and rows are multiples of
+ * 16 bytes.
+ *
+ * vit_pages_attend: rows query_offsets[r] ... query_offsets[r + 1] - 1 of q and out are request r's; row i's head h (at
+ * i * stride + h * head_dim) attends to its request's kv_lens[r] keys of head h / (q_heads / kv_heads):
+ *   out = sum_j softmax_j(scale * q . k_j) v_j,
+ * over all keys, or with `causal` over those up to its own, where the request's rows are the last of its keys.  A row
+ * that sees no key gets zeros.  What no row may see (keys past kv_lens or past a row's own, other pages, pages whose number
+ * lies outside 0 ... n_pages - 1) has no effect, infinities and NaN among it.  Rows behind the last request's are left as they
+ * are.  max_new: no request has more rows (of one that has, those past max_new are left as they are).  Logits, softmax and
+ * sums are fp32; in bf16 the weights are rounded to bf16 ahead of the second product.  The keys' axis is divided
+ * by what the batch leaves of the device, so the last bits of a row depend on the batch, never on timing.
+ * head_dim is a multiple of 8, at most 128; q_heads a multiple of kv_heads; scale finite; pointers and rows multiples of 16 bytes.
+ * vit_pages_attend_query: bytes of workspace that the call needs (pointers in the struct are not looked at); the workspace is
+ * 256-byte aligned, its contents undefined before and after, and no two calls at work at a time may share it.
+ * Errors: VIT_EINVAL (NULL, sizes, alignment), VIT_ECAPACITY (workspace), VIT_EDEVICE; nothing was launched.
+ */
+typedef struct {
+  const int32_t* cached_lens;
+  const int32_t* new_lens;
+  int32_t* block_table; /* [n_requests, table_width], rows table_stride entries apart */
+  const int32_t* free_pages;
+  const int32_t* taken;
+  int32_t* slots;
+  int32_t* query_offsets;
+  int32_t* kv_lens;
+  int32_t* page_offsets;
+  int32_t* counts;
+  int64_t table_stride;
+  int32_t n_requests; /* at most 2^20 */
+  int32_t table_width;
+  int32_t n_free;
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t n_rows; /* below 2^30 */
+} vit_pages_plan_t;
+
+typedef struct {
+  const void* k;
+  const void* v;
+  const int32_t* slots;
+  void* key_pages;
+  void* value_pages;
+  int64_t k_stride; /* elements from a row to the next */
+  int64_t v_stride;
+  int32_t n_rows;
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t kv_heads;
+  int32_t head_dim;
+  int32_t dtype; /* VIT_DTYPE_* */
+} vit_pages_append_t;
+
+typedef struct {
+  const void* q;
+  const void* key_pages;
+  const void* value_pages;
+  const int32_t* block_table; /* [n_requests, table_width], rows table_stride entries apart */
+  const int32_t* query_offsets;
+  const int32_t* kv_lens;
+  void* out;
+  void* workspace;
+  size_t workspace_bytes;
+  int64_t q_stride; /* elements from a row to the next */
+  int64_t out_stride;
+  int64_t table_stride;
+  int32_t n_rows; /* rows that q and out hold */
+  int32_t n_requests;
+  int32_t max_new;
+  int32_t table_width;
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t q_heads; /* at most 1024 */
+  int32_t kv_heads;
+  int32_t head_dim;
+  int32_t causal;
+  int32_t dtype; /* VIT_DTYPE_* */
+  float scale;
+} vit_pages_attend_t;
+
+vit_status_t vit_pages_plan(const vit_pages_plan_t* args, void* stream);
+vit_status_t vit_pages_append(const vit_pages_append_t* args, void* stream);
+vit_status_t vit_pages_attend_query(const vit_pages_attend_t* args, size_t* workspace_bytes);
+vit_status_t vit_pages_attend(const vit_pages_attend_t* args, void* stream);
+
+/*
  * Measurement aid (no part of the encode path): runs a register-only bf16 MFMA loop
  * (v_mfma_f32_32x32x16_bf16, two waves per SIMD, no memory traffic) on `device` for about
  * `seconds` (0 < seconds <= 2) on the null stream and writes the sustained rate in TFLOP/s

@@ -24,3 +24,4 @@ from .binding import (  # noqa: F401
     vit_product_time,
     vit_weight_count,
 )
+from .pages import PagePlan, append_pages, attend_pages, plan_pages  # noqa: F401

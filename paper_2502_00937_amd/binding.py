@@ -91,6 +91,11 @@ def load_library():
     lib.vit_preprocess_tiles.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                          C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
                                          C.c_void_p]
+    for call in (lib.vit_pages_plan, lib.vit_pages_append, lib.vit_pages_attend):  # (the struct's bytes, the stream)
+        call.restype = C.c_int
+        call.argtypes = [C.c_void_p, C.c_void_p]
+    lib.vit_pages_attend_query.restype = C.c_int
+    lib.vit_pages_attend_query.argtypes = [C.c_void_p, C.POINTER(C.c_size_t)]
     lib.vit_mfma_ceiling.restype = C.c_int
     lib.vit_mfma_ceiling.argtypes = [C.c_int, C.c_double, C.c_int32, C.POINTER(C.c_double)]
     lib.vit_product_plan.restype = C.c_int

@@ -1,0 +1,527 @@
+"""The paged cache's operators against plain implementations in 64 bits and whole numbers."""
+import numpy as np
+import pytest
+
+from parity_util import say
+
+pytestmark = pytest.mark.gpu
+
+
+def dev(values):
+    import torch
+
+    return torch.tensor(np.asarray(values), dtype=torch.int32, device="cuda")
+
+
+# ---- plan ---------------------------------------------------------------------------------
+def plain_plan(cached, new, table, free, taken, n_pages, page, rows):
+    table, slots, starts, kv, firsts, lost = table.copy(), [], [0], [], [max(taken, 0)], 0
+    taken = max(taken, 0)
+    for r, (c, n) in enumerate(zip(cached, new)):
+        c, n = max(c, 0), max(n, 0)
+        fits = min(n, rows - len(slots))
+        lost += n - fits
+        for at in range(c, c + fits):
+            nth = at // page
+            if nth < table.shape[1] and at % page == 0:
+                table[r, nth] = free[taken] if taken < len(free) and 0 <= free[taken] < n_pages else -1
+                taken += 1
+            number = table[r, nth] if nth < table.shape[1] else -1
+            slots.append(number * page + at % page if 0 <= number < n_pages else -1)
+            lost += slots[-1] < 0
+        starts.append(starts[-1] + fits)
+        kv.append(c + fits)
+        firsts.append(taken)
+    slots += [-1] * (rows - len(slots))
+    return slots, starts, kv, firsts, [min(taken, len(free)), lost], table
+
+
+def some_lengths(seed, n, top_cached, top_new):
+    rng = np.random.default_rng(seed)
+    return rng.integers(0, top_cached + 1, n).tolist(), rng.integers(0, top_new + 1, n).tolist()
+
+
+PLANS = {
+    "one token": ([0], [1], 16, 4, 0, 0),
+    "one token in an open page": ([17], [1], 16, 4, 0, 0),
+    "no request": ([], [], 8, 3, 0, 2),
+    "requests without tokens around one": ([5, 0, 0, 31, 8], [0, 0, 33, 0, 0], 8, 9, 0, 0),
+    "no token at all": ([5, 7], [0, 0], 8, 2, 0, 0),
+    "pages that end with the step": ([8, 16, 0], [8, 16, 24], 8, 6, 0, 0),
+    "negative lengths": ([-3, 4], [5, -7], 8, 3, 0, 0),
+    "a workgroup's requests and one": (*some_lengths(1, 1025, 300, 2), 64, 8, 0, 3),
+    "several times a workgroup's": (*some_lengths(2, 3000, 90, 40), 16, 10, 0, 0),
+    "long ones": (*some_lengths(3, 7, 3000, 5000), 128, 70, 0, 60),
+    "wide pages": (*some_lengths(4, 11, 9000, 6000), 4096, 5, 0, 0),
+    "rows for fewer": ([3, 60, 8, 1], [20, 50, 9, 4], 8, 20, -25, 0),
+    "rows for none": ([3], [20], 8, 20, -20, 0),
+}
+
+
+@pytest.mark.parametrize("name", PLANS)
+@pytest.mark.parametrize("trouble", ["", "table", "list", "numbers"])
+def test_plan(name, trouble):
+    """Whole numbers, equal to a loop over the tokens; with a table or a free list that is too short, or numbers outside the
+    pool in both."""
+    import paper_2502_00937_amd as V
+
+    say(f"case plan: {name}, {trouble or 'no trouble'}")
+    cached, new, page, width, extra, taken = PLANS[name]
+    rng = np.random.default_rng(len(name))
+    rows = sum(max(n, 0) for n in new) + extra + (7 if extra == 0 else 0)
+    if trouble == "table":
+        width = max(1, width // 2)
+    n_pages = width * len(cached) + taken + 40
+    order = rng.permutation(n_pages)
+    table = order[rng.integers(0, n_pages, (len(cached), width))].astype(np.int64)
+    free = order[:n_pages if trouble != "list" else taken + 3].astype(np.int64)
+    if trouble == "numbers":
+        free[::3] = -4
+        free[1::7] = n_pages
+        table[:, ::2] = 2 ** 31 - 1
+    want = plain_plan(cached, new, table, free, taken, n_pages, page, rows)
+    t = dev(np.pad(table, ((0, 0), (0, 5)), constant_values=-77)).reshape(len(cached), width + 5)
+    plan = V.plan_pages(dev(cached), dev(new), t[:, :width], dev(free), dev([taken, 99]), n_pages, page, rows)
+    for field, got, w in zip(plan._fields, plan, want):
+        assert got.tolist() == list(w), field
+    assert t[:, :width].tolist() == want[5].tolist() and (t[:, width:] == -77).all()
+
+
+def test_plan_of_a_step_that_is_repeated_in_place():
+    """kv_lens over cached_lens and counts over taken, eagerly and from a graph: every replay is the next step."""
+    import torch
+
+    import paper_2502_00937_amd as V
+
+    rng = np.random.default_rng(5)
+    n, page, width, steps = 40, 8, 12, 7
+    cached = rng.integers(0, 30, n)
+    n_pages = n * width
+    order = rng.permutation(n_pages)
+    table, at = np.full((n, width), -1), 0
+    for r in range(n):
+        held = -(-cached[r] // page)
+        table[r, :held] = order[at:at + held]
+        at += held
+    new = rng.integers(0, 4, n)
+    rows = int(new.sum()) + 3
+    free = order[at:]
+    lens, counts, t, d_new, d_free = dev(cached), dev([0, 0]), dev(table), dev(new), dev(free)
+    plan = V.PagePlan(dev([0] * rows), dev([0] * (n + 1)), lens, dev([0] * (n + 1)), counts)
+
+    def step():
+        V.plan_pages(lens, d_new, t, d_free, counts, n_pages, page, rows, out=plan)
+
+    graph, taken = torch.cuda.CUDAGraph(), 0
+    for i in range(steps):
+        if i == 2:
+            torch.cuda.synchronize()
+            with torch.cuda.graph(graph):
+                step()
+        if i < 2:
+            step()
+        else:
+            graph.replay()
+        torch.cuda.synchronize()
+        torch.ones(1000, device="cuda").sum().item()
+        slots, starts, cached, firsts, total, table = plain_plan(cached, new, table, free, taken, n_pages, page, rows)
+        taken = total[0]
+        assert plan.slots.tolist() == slots and lens.tolist() == cached and counts.tolist() == total and t.tolist() == table.tolist()
+
+
+# ---- append -------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,heads,dim,page", [(1, 1, 8, 8), (3, 2, 64, 16), (257, 8, 128, 32), (1000, 3, 72, 64), (37, 5, 80, 8), (130, 40, 128, 16)])
+def test_append(dtype, rows, heads, dim, page):
+    import torch
+
+    import paper_2502_00937_amd as V
+
+    say(f"case append: {rows} rows of {heads} x {dim} {dtype}, pages of {page}")
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator().manual_seed(rows)
+    pages = -(-rows // page) + 3
+    fused = torch.randn(rows, 4 * heads + 1, dim, generator=g).to(dt)
+    k, v = fused[:, heads:2 * heads], fused[:, 2 * heads + 1:3 * heads + 1]
+    slots = torch.randperm(pages * page, generator=g)[:rows].to(torch.int32)
+    if rows > 2:
+        slots[rows // 2] = -1
+        slots[1] = -2 ** 31
+        slots[rows - 1] = pages * page
+    old = torch.randn(2, pages, heads, page, dim, generator=g).to(dt)
+    want = old.clone()
+    for i, s in enumerate(slots.tolist()):
+        if 0 <= s < pages * page:
+            want[0, s // page, :, s % page] = k[i]
+            want[1, s // page, :, s % page] = v[i]
+    d, f = old.cuda(), fused.cuda()
+    V.append_pages(f[:, heads:2 * heads], f[:, 2 * heads + 1:3 * heads + 1], slots.cuda(), d[0], d[1])
+    assert torch.equal(d.cpu(), want)
+
+
+# ---- attend -------------------------------------------------------------------------------
+def make_case(dtype, heads, kv_heads, dim, page, lens, seed=0, garbage=True, spread=2.0, extra_rows=0):
+    """Pools, block table, lengths and queries of requests with `lens` = [(new, keys)].  What nobody may see is NaN, infinity or the
+    largest number of its kind: other pages, the last page's rest, the table's rest."""
+    import torch
+
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(seed + 1)
+    width = max([1] + [-(-k // page) for _, k in lens]) + 2
+    need = sum(-(-k // page) for _, k in lens)
+    n_pages = need + 4
+    order = torch.randperm(n_pages, device="cuda", generator=g).to(torch.int32)
+    pools = torch.randn(2, n_pages, kv_heads, page, dim, device="cuda", generator=g).to(dt)
+    kept = torch.zeros(n_pages, page, dtype=torch.bool, device="cuda")
+    table = torch.empty(len(lens), width, dtype=torch.int32, device="cuda")
+    table[:, ::3], table[:, 1::3], table[:, 2::3] = -5, 2 ** 31 - 1, n_pages
+    at = 0
+    for r, (_, keys) in enumerate(lens):
+        count = -(-keys // page)
+        table[r, :count] = order[at:at + count]
+        numbers = order[at:at + count].long()
+        kept[numbers] = (torch.arange(count * page, device="cuda") < keys).view(count, page)
+        at += count
+    if garbage:
+        bad = torch.tensor([float("nan"), float("inf"), -float("inf"), torch.finfo(dt).max, torch.finfo(dt).min], device="cuda").to(dt)
+        lost = ~kept[None, :, None, :, None].expand(pools.shape)
+        pools = torch.where(lost, bad[torch.randint(0, 5, pools.shape, device="cuda", generator=g)], pools).contiguous()
+    starts = np.concatenate([[0], np.cumsum([n for n, _ in lens])])
+    rows = int(starts[-1]) + extra_rows
+    q = (torch.randn(rows, heads + 3, dim, device="cuda", generator=g) * spread).to(dt)[:, 2:heads + 2]
+    return dict(q=q, key_pages=pools[0], value_pages=pools[1], block_table=table, query_offsets=dev(starts), kv_lens=dev([k for _, k in lens]),
+                max_new=max([1] + [n for n, _ in lens]))
+
+
+def plain_attend(c, lens, causal, scale):
+    """(values, tolerances) in 64 bits, request by request over what its rows may see alone.
+
+    With u the rounding of the type: a weight rounded to bf16 is off by u of itself at most, the sums of weights being of the
+    same rounded ones, so the result by u * sum w |v - out| <= 2 u sum w |v|.  A logit is the fp32 sum of dim products and a
+    multiplication with the scale (and with log2 e), off by (dim + 4) 2^-24 of sum |q k| scale; the exponential's own
+    error is a few 2^-24 of it more: for an argument x, exp2 sees x rounded, |x| 2^-24.  The weights' sums and the products'
+    run over at most all keys in fp32: keys * 2^-24 of sum w |v|, twice, and the joining of parts a few more.  The
+    output's rounding is u |out|."""
+    import torch
+
+    u = torch.finfo(c["q"].dtype).eps / 2
+    weights_u = u if c["q"].dtype == torch.bfloat16 else 0.0
+    heads, kv_heads, page = c["q"].shape[1], c["key_pages"].shape[1], c["key_pages"].shape[2]
+    group, dim = heads // kv_heads, c["q"].shape[2]
+    n_pages = c["key_pages"].shape[0]
+    out, tol = [], []
+    first = 0
+    for r, (new, keys) in enumerate(lens):
+        x = c["q"][first:first + new].double()
+        first += new
+        o, t = torch.zeros_like(x), torch.zeros_like(x)
+        at = torch.arange(keys, device=x.device)
+        numbers = c["block_table"][r].long()[at // page]
+        held = (numbers >= 0) & (numbers < n_pages)
+        k, v = (p[numbers.clamp(0, n_pages - 1), :, at % page].double() for p in (c["key_pages"], c["value_pages"]))
+        if keys and new and bool(held.any()):
+            k, v, at = k[held], v[held], at[held]
+            rows = torch.arange(new, device=x.device)[:, None]
+            seen = (at <= keys - new + rows if causal else at >= 0 * rows).repeat_interleave(group, 0)  # [new * group, keys]
+            n = seen.sum(1, keepdim=True)
+            for h in range(kv_heads):
+                qs = x[:, h * group:(h + 1) * group].reshape(-1, dim)
+                logits = (qs @ k[:, h].T.contiguous() * scale).masked_fill(~seen, -torch.inf)
+                w = torch.softmax(logits, 1).masked_fill(n == 0, 0.0)
+                y, mass = w @ v[:, h], w @ v[:, h].abs()
+                size = (qs.abs() @ k[:, h].abs().T.contiguous() * abs(scale)).masked_fill(~seen, 0.0).amax(1, keepdim=True)
+                off = 2 * weights_u + 2 * ((dim + 8) * 2.0 ** -24 * size) + (2 * n + 64) * 2.0 ** -24
+                o[:, h * group:(h + 1) * group] = y.view(new, group, dim)
+                t[:, h * group:(h + 1) * group] = (off * mass + u * y.abs()).view(new, group, dim)
+        out.append(o)
+        tol.append(t)
+    return torch.cat(out), torch.cat(tol)
+
+
+def compare(got, want, tol, what):
+    import torch
+
+    assert got.shape == want.shape
+    err = (got.double() - want).abs()
+    assert torch.isfinite(got).all(), what
+    worst = float((err / tol.clamp(min=1e-300)).nan_to_num(0.0).max()) if err.numel() else 0.0
+    say(f"    {what}: largest error {worst:.3f} of its bound")
+    assert bool((err <= tol).all()), what
+
+
+HEADS = [(8, 2, 128), (4, 4, 64), (6, 1, 80), (9, 3, 72), (4, 2, 96), (3, 1, 8), (7, 1, 128), (32, 1, 64), (2, 2, 120), (64, 1, 32)]
+LENS = {
+    "single tokens": [(1, 1), (1, 9), (1, 63), (1, 64), (1, 65), (1, 400), (1, 0), (1, 1601)],
+    "a few tokens": [(2, 2), (3, 200), (5, 130), (4, 33)],
+    "chunks": [(17, 64), (0, 50), (130, 130), (33, 1000), (1, 700), (64, 320)],
+    "odd ones": [(0, 0), (3, 2), (127, 129), (0, 0), (1, 1), (255, 255), (2, 0)],
+    "one long": [(1, 9000)],
+    "one chunk": [(300, 2500)],
+}
+
+
+def check(c, lens, causal, scale=None, what=""):
+    import paper_2502_00937_amd as V
+
+    got = V.attend_pages(**c, causal=causal, scale=scale)
+    rows = sum(n for n, _ in lens)
+    want, tol = plain_attend(c, lens, causal, c["q"].shape[2] ** -0.5 if scale is None else scale)
+    compare(got[:rows], want, tol, what)
+
+
+@pytest.mark.parametrize("name", LENS)
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,kv_heads,dim", HEADS)
+def test_attend(name, dtype, causal, heads, kv_heads, dim):
+    page = {8: 8, 72: 16, 80: 64, 96: 32, 120: 128}.get(dim, 16)
+    say(f"case attend: {name}, {dtype}, causal {causal}, {heads} / {kv_heads} heads of {dim}, pages of {page}")
+    c = make_case(dtype, heads, kv_heads, dim, page, LENS[name], seed=dim)
+    check(c, LENS[name], causal, what=f"{name} {dtype}")
+
+
+@pytest.mark.parametrize("page", [8, 16, 32, 64, 128, 4096])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_attend_page_sizes(page, dtype):
+    lens = [(1, 5000), (70, 333), (2, 129), (1, page), (1, page + 1)]
+    say(f"case attend: pages of {page}, {dtype}")
+    check(make_case(dtype, 8, 2, 64, page, lens), lens, True, what=f"pages of {page}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("spread,scale", [(0.0, None), (40.0, None), (2.0, 1.0), (2.0, -0.3), (2.0, 0.0), (300.0, 1.0)])
+@pytest.mark.parametrize("lens", [[(1, 2000), (1, 70)], [(150, 700), (9, 9)]], ids=["tokens", "chunks"])
+def test_attend_logits_of_any_size(dtype, spread, scale, lens):
+    """All equal, hundreds apart, the other way round: weights that underflow, a maximum that moves."""
+    say(f"case attend: queries of {spread}, scale {scale}, {dtype}")
+    check(make_case(dtype, 4, 2, 128, 16, lens, spread=spread), lens, True, scale, what=f"spread {spread} scale {scale}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens", [[(1, 3000)], [(40, 500), (1, 64)]], ids=["tokens", "chunks"])
+def test_attend_rising_logits(dtype, lens):
+    """Keys along the query, longer and longer: every tile's logits outgrow all those before it."""
+    import torch
+
+    c = make_case(dtype, 2, 1, 64, 16, lens)
+    c["q"] = torch.ones_like(c["q"])
+    for r, (_, keys) in enumerate(lens):
+        at = torch.arange(keys, device="cuda")
+        rising = (at.float() * 0.05 - 30).to(c["q"].dtype)
+        c["key_pages"][c["block_table"][r].long()[at // 16], 0, at % 16] = rising[:, None].expand(keys, 64)
+    check(c, lens, True, what="rising")
+    c["q"] = -c["q"]
+    check(c, lens, True, what="falling")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens", [[(6, 40), (50, 70)], [(200, 200)], [(2, 1000), (1, 300)]])
+def test_attend_later_values_that_are_no_numbers(dtype, lens):
+    """Keys and values of a request's last token are NaN or infinite: rows before it do not see them."""
+    import torch
+
+    import paper_2502_00937_amd as V
+
+    for value in (float("nan"), float("inf"), -float("inf")):
+        c = make_case(dtype, 4, 2, 128, 16, lens)
+        clean, tol = plain_attend(c, lens, True, 128 ** -0.5)
+        last = [sum(n for n, _ in lens[:r + 1]) - 1 for r in range(len(lens))]
+        for r, (_, keys) in enumerate(lens):
+            page, at = int(c["block_table"][r, (keys - 1) // 16]), (keys - 1) % 16
+            c["value_pages"][page, :, at, ::3] = value
+            c["key_pages"][page, :, at] = value
+        got = V.attend_pages(**c)
+        others = [i for i in range(got.shape[0]) if i not in last]
+        compare(got[others], clean[others], tol[others], f"last token {value}")
+        assert not torch.isfinite(got[last]).all(-1).any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_attend_pages_outside_the_pool(dtype):
+    """Numbers outside the pool in the middle of a block table hide their keys, all of a request's too."""
+    lens = [(1, 400), (60, 300), (1, 100), (5, 90), (1, 2000)]
+    c = make_case(dtype, 8, 2, 64, 16, lens)
+    c["block_table"][0, 3], c["block_table"][0, 24], c["block_table"][1, 0:5] = -1, 2 ** 31 - 1, c["key_pages"].shape[0]
+    c["block_table"][1, 17], c["block_table"][2, :], c["block_table"][3, 2:4] = -2 ** 31, -1, -9
+    c["block_table"][4, ::2] = -1
+    for causal in (True, False):
+        check(c, lens, causal, what=f"bad pages, causal {causal}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_attend_writes_its_rows_alone(dtype):
+    """Rows behind the last request's, rows past max_new and what lies between two rows of `out` stay as they were."""
+    import torch
+
+    import paper_2502_00937_amd as V
+
+    lens = [(3, 50), (40, 90), (1, 7)]
+    c = make_case(dtype, 6, 2, 72, 16, lens, extra_rows=5)
+    want, tol = plain_attend(c, lens, True, 72 ** -0.5)
+    buf = torch.full((49, 11, 72), 123.0, dtype=c["q"].dtype, device="cuda")
+    out = V.attend_pages(**c, out=buf[:, 2:8])
+    assert out.data_ptr() == buf[:, 2:8].data_ptr()
+    compare(buf[:44, 2:8], want, tol, "rows")
+    assert (buf[44:] == 123).all() and (buf[:, :2] == 123).all() and (buf[:, 8:] == 123).all()
+    buf.fill_(123.0)
+    V.attend_pages(**dict(c, max_new=17), out=buf[:, 2:8])
+    rows = list(range(20)) + [43]
+    compare(buf[rows, 2:8], want[rows], tol[rows], "rows up to max_new")
+    assert (buf[20:43] == 123).all() and (buf[44:] == 123).all()
+    assert V.attend_pages(**dict(c, q=c["q"][:0])).shape == (0, 6, 72)
+
+
+def test_attend_many_requests():
+    lens = [(1, 1 + (37 * i) % 211) for i in range(1500)] + [(3, 40)]
+    check(make_case("bf16", 4, 2, 64, 16, lens), lens, True, what="1501 requests")
+
+
+def test_offsets_past_32_bits():
+    """Pools of more than 2^32 bytes and 2^31 values: pages at both ends."""
+    import torch
+
+    import paper_2502_00937_amd as V
+
+    n_pages, heads, page, dim = 140000, 8, 16, 128
+    pools = [torch.zeros(n_pages, heads, page, dim, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    assert pools[0].numel() > 2 ** 31
+    lens = [(1, 100), (90, 150)]
+    c = make_case("bf16", 16, 8, dim, page, lens, garbage=False)
+    used = c["block_table"].clone()
+    far = [0, n_pages - 1] + [n_pages - 2 - i if i % 2 else i for i in range(1, 40)]
+    k = 0
+    for r, (_, keys) in enumerate(lens):
+        for i in range(-(-keys // page)):
+            for pool, small in zip(pools, (c["key_pages"], c["value_pages"])):
+                pool[far[k]] = small[used[r, i]]
+            used[r, i] = far[k]
+            k += 1
+    small = V.attend_pages(**c)
+    got = V.attend_pages(**dict(c, key_pages=pools[0], value_pages=pools[1], block_table=used))
+    assert torch.equal(got, small)
+    rows = torch.randn(3, 2 * heads, dim, device="cuda").to(torch.bfloat16)
+    slots = dev([0, n_pages * page - 1, (n_pages - 5) * page + 3])
+    V.append_pages(rows[:, :heads], rows[:, heads:], slots, *pools)
+    for i, s in enumerate(slots.tolist()):
+        assert torch.equal(pools[0][s // page, :, s % page], rows[i, :heads]) and torch.equal(pools[1][s // page, :, s % page], rows[i, heads:])
+
+
+def test_attend_on_other_streams_and_in_graphs():
+    """Two calls at once on two streams, and two graphs replayed in turn with eager work between: the eager call's bits."""
+    import torch
+
+    import paper_2502_00937_amd as V
+
+    cases = [make_case("bf16", 8, 2, 128, 16, lens, seed=i) for i, lens in enumerate(([(1, 4000), (1, 90)], [(120, 900), (1, 50)]))]
+    want = [V.attend_pages(**c) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [torch.empty_like(w) for w in want]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, c, g in zip(streams, cases, got):
+            with torch.cuda.stream(s):
+                V.attend_pages(**c, out=g)
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, w) for g, w in zip(got, want))
+    graphs = [torch.cuda.CUDAGraph() for _ in cases]
+    for graph, c, g in zip(graphs, cases, got):
+        with torch.cuda.graph(graph):
+            V.attend_pages(**c, out=g)
+    for i in range(4):
+        for c in cases:  # other values of the same batch
+            c["q"].copy_(torch.randn(c["q"].shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(i)))
+        for graph, g in zip(graphs, got):
+            g.fill_(float("nan"))
+            graph.replay()
+        torch.cuda.synchronize()
+        for c, g in zip(cases, got):
+            assert torch.equal(V.attend_pages(**c), g)
+
+
+# ---- together -----------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_requests_from_prompt_to_tokens(dtype):
+    """Prompts in ragged chunks, then single tokens, several requests a step, pages taken as they fill: every step's rows against
+    causal attention over all of their request so far."""
+    import torch
+
+    import paper_2502_00937_amd as V
+
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(11)
+    heads, kv_heads, dim, page, n = 6, 2, 80, 16, 4
+    pools = [torch.full((60, kv_heads, page, dim), float("nan"), dtype=dt, device="cuda") for _ in range(2)]
+    table, free = torch.full((n, 16), -1, dtype=torch.int32, device="cuda"), torch.randperm(60, device="cuda", generator=g).to(torch.int32)
+    lens, taken = dev([0] * n), None
+    history = [[], [], [], []]
+    for step, new in enumerate(([70, 0, 33, 1], [40, 129, 1, 1], [1, 1, 1, 1], [1, 1, 0, 1], [1, 20, 1, 1])):
+        rows = sum(new) + 3  # a padded batch
+        qkv = torch.randn(rows, heads + 2 * kv_heads, dim, device="cuda", generator=g).to(dt)
+        q, k, v = qkv[:, :heads], qkv[:, heads:heads + kv_heads], qkv[:, heads + kv_heads:]
+        plan = V.plan_pages(lens, dev(new), table, free, taken, 60, page, rows)
+        V.append_pages(k, v, plan.slots, *pools)
+        out = torch.full((rows, heads, dim), 5.0, dtype=dt, device="cuda")
+        V.attend_pages(q, *pools, table, plan.query_offsets, plan.kv_lens, max(new), out=out)
+        lens, taken = plan.kv_lens, plan.counts
+        assert int(plan.counts[1]) == 0
+        at = 0
+        for r, m in enumerate(new):
+            history[r].append((k[at:at + m], v[at:at + m]))
+            ks, vs = (torch.cat(x) for x in zip(*history[r]))
+            if m:
+                # the request alone, in a cache of one page after another
+                c = dict(q=q[at:at + m], block_table=torch.arange(40, dtype=torch.int32, device="cuda")[None], kv_lens=dev([len(ks)]))
+                for name, x in (("key_pages", ks), ("value_pages", vs)):
+                    flat = torch.zeros(40 * 8, kv_heads, dim, dtype=dt, device="cuda")
+                    flat[:len(x)] = x
+                    c[name] = flat.view(40, 8, kv_heads, dim).transpose(1, 2).contiguous()
+                want, tol = plain_attend(c, [(m, len(ks))], True, dim ** -0.5)
+                compare(out[at:at + m], want, tol, f"step {step} request {r}")
+            at += m
+        assert (out[at:] == 5).all()
+
+
+def test_text_over_encoded_images():
+    """Encoder, hand-off, keys and values of the pulled tokens into pages, text of each request over its own images: a request
+    without images sees nothing."""
+    import torch
+
+    import gen
+    import paper_2502_00937_amd as V
+
+    cfg = gen.get_config("test_small_bf16")
+    enc = V.VitEncoder(cfg, gen.make_weights(cfg, seed=0), device=0)
+    try:
+        images = [2, 0, 1]
+        tokens, offsets = enc.encode(torch.from_numpy(gen.make_pixels(cfg, 4, seed=1)).cuda(), images, [0, 2, 3, 4])
+        width, heads, kv_heads, dim, page = tokens.shape[1], 4, 2, 64, 8
+        g = torch.Generator(device="cuda").manual_seed(3)
+        weight = torch.randn(width, 2 * kv_heads * dim, device="cuda", generator=g) * width ** -0.5
+        hand = V.TokenHandoff(0)
+        stream = torch.cuda.current_stream().cuda_stream
+        pulled = torch.empty_like(tokens)
+        bounds = [int(o) for o in offsets]
+        for r in range(3):
+            if images[r]:
+                hand.expect(r, 1)
+                part = tokens[bounds[r]:bounds[r + 1]]
+                hand.publish(r, 0, part.data_ptr(), part.numel() * 2, stream)
+                to = pulled[bounds[r]:bounds[r + 1]]
+                hand.pull(r, to.data_ptr(), to.numel() * 2, stream)
+                hand.release(r)
+        hand.close()
+        counts = [b - a for a, b in zip(bounds, bounds[1:])]
+        kv = (pulled.float() @ weight).to(torch.bfloat16).view(-1, 2 * kv_heads, dim)
+        pools = [torch.full((24, kv_heads, page, dim), float("inf"), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        table = torch.full((3, 12), -1, dtype=torch.int32, device="cuda")
+        plan = V.plan_pages(dev([0, 0, 0]), dev(counts), table, torch.arange(23, -1, -1, device="cuda", dtype=torch.int32), None, 24, page, len(kv))
+        assert plan.query_offsets.tolist() == bounds and int(plan.counts[1]) == 0
+        V.append_pages(kv[:, :kv_heads], kv[:, kv_heads:], plan.slots, *pools)
+        text = [5, 3, 1]
+        lens = list(zip(text, counts))
+        c = dict(q=torch.randn(9, heads, dim, device="cuda", generator=g).to(torch.bfloat16), key_pages=pools[0], value_pages=pools[1],
+                 block_table=table, query_offsets=dev([0, 5, 8, 9]), kv_lens=plan.kv_lens, max_new=5)
+        check(c, lens, False, what="text over images")
+        assert (V.attend_pages(**c, causal=False)[5:8] == 0).all()
+    finally:
+        enc.close()
