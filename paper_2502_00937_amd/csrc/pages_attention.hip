@@ -42,8 +42,8 @@ struct PagedArgs {
   int64_t max_parts;
   int64_t q_stride, out_stride, table_stride;
   int rows, R, max_new, width, n_pages, shift, heads, kv_heads, group, dh, causal;
-  int target;    // workgroups to divide the keys for, 0: not at all
-  int least;     // key tiles that are not divided further
+  int divide;    // whether keys are divided
+  int slots;     // logarithm of the workgroups that the device holds at a time, which they are divided for
   int part_rows; // rows of a part
   float scale;   // >= 0, times log2(e)
   int negative;  // the scale's sign, which goes to the queries
@@ -60,22 +60,25 @@ struct Shape {
   static constexpr int ROWB = DB * 32 * ES <= 128 ? 128 : DB * 32 * ES <= 256 ? 256 : 512;  // bytes of a row in LDS
   static constexpr int CPR = ROWB / 16, RPI = 64 / CPR;      // 16-byte pieces of a row; rows that a load instruction fills
   static constexpr int KS = DB * 32 * ES / 32;               // pairs of pieces that the first product runs over
-  static constexpr int TK = ES == 2 ? 64 : 32;               // WIDE: keys of a tile
-  static constexpr int KEYS = NARROW ? 32 : TK;              // keys that a wave works on at a time
-  static constexpr int LOAD = NARROW ? 32 : TK / 4;          // of them, keys that it loads
+  static constexpr int KEYS = NARROW ? 32 : 64;              // keys that a wave works on at a time
+  static constexpr int LOAD = NARROW ? 32 : 16;              // of them, keys that it loads
   static constexpr int INSTR = LOAD / RPI;                   // load instructions for K, and for V
   static constexpr int PAGES = LOAD / 8;                     // pages it looks up
-  static constexpr int STAGE = KEYS * ROWB * 2;              // bytes of LDS of a stage
-  static constexpr int NS = NARROW && 8 * STAGE > 131072 ? 1 : 2;
-  static constexpr int LDS = (NARROW ? 4 : 1) * NS * STAGE;
+  static constexpr int TILE = KEYS * ROWB;                   // bytes of LDS of a tile of K or V
+  // NARROW: tiles on their way at a time, of K and of V, for each wave.  (WIDE: two of either.)
+  static constexpr int NS = NARROW && ES == 4 ? 1 : 2;
+  static constexpr int LDS = (NARROW ? 4 : 1) * NS * 2 * TILE;
   static constexpr int ITEM_ROWS = NARROW ? 32 : 128;
-  static constexpr int ITEM_KEYS = NARROW ? 128 : TK;        // keys of a step of the whole workgroup
+  static constexpr int ITEM_KEYS = NARROW ? 128 : 64;        // keys of a step of the whole workgroup
 };
 
 // ---- a workgroup's place ------------------------------------------------------------------
 struct Item {
-  int r, tile, split, splits, part;  // request; which of its row tiles, which part of its keys and of how many; first part's place
-  int start, fresh, kv, rows;        // its first row, rows, keys; rows of (request, head of keys)
+  int r, tile;                 // request, and which of its row tiles
+  int split, splits;           // WIDE: which part of its keys, of how many
+  int first, last;             // NARROW: which steps of its keys
+  int part;                    // where its results go if they are a part (WIDE: the request's first part), else -1
+  int start, fresh, kv, rows;  // the request's first row, rows, keys; rows of (request, head of keys)
 };
 
 struct Request {
@@ -91,7 +94,8 @@ __device__ __forceinline__ Request request(const PagedArgs& a, int r) {
     q.fresh = q.start < 0 || n < 0 || q.start + n > a.rows ? 0 : (int)n;
     q.kv = max(a.kv[r], 0);
     q.tiles = (int)(((int64_t)min(q.fresh, a.max_new) * a.group + ROWS - 1) / ROWS);
-    q.steps = (int)((min((int64_t)q.kv, (int64_t)a.width << a.shift) + KEYS - 1) / KEYS);
+    // (at least one: rows that see nothing have to be written)
+    q.steps = max((int)((min((int64_t)q.kv, (int64_t)a.width << a.shift) + KEYS - 1) / KEYS), 1);
   }
   return q;
 }
@@ -106,16 +110,16 @@ __device__ __forceinline__ int64_t wave_scan(int64_t v) {
   return v;
 }
 
-// Workgroup `at` of a head of keys, in the order of the requests; false if there are not so many.
+// WIDE: workgroup `at` of a head of keys, in the order of the requests, into `found` in LDS; false if there are not so many.
 template <int ROWS, int KEYS>
-__device__ __forceinline__ bool find_item(const PagedArgs& a, int at, Item& it) {
+__device__ __forceinline__ bool find_item(const PagedArgs& a, int at, Item& found) {
   __shared__ int64_t sums[4];
-  __shared__ Item found;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int64_t share = INT32_MAX;
-  if (a.target) {
-    int64_t work = 0;
-    for (int r = tid; r < a.R; r += THREADS) {
+  int share = INT32_MAX;
+  const Request head = request<ROWS, KEYS>(a, tid);
+  if (a.divide) {
+    int64_t work = (int64_t)head.tiles * head.steps;
+    for (int r = tid + THREADS; r < a.R; r += THREADS) {
       const Request q = request<ROWS, KEYS>(a, r);
       work += (int64_t)q.tiles * q.steps;
     }
@@ -125,13 +129,13 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int at, Item& it) 
     __syncthreads();
     work = (sums[0] + sums[1] + sums[2] + sums[3]) * a.kv_heads;
     __syncthreads();
-    share = max((work + a.target - 1) / a.target, (int64_t)a.least);
+    share = (int)min(max((work + (1 << a.slots) - 1) >> a.slots, (int64_t)1), (int64_t)INT32_MAX);
   }
   if (tid == 0) found.r = -1;
   int64_t below = 0;  // places of the requests before, parts of those among them whose keys are divided in the upper half
   for (int base = 0; base < a.R; base += THREADS) {
-    const Request q = request<ROWS, KEYS>(a, base + tid);
-    const int splits = q.steps > share ? (int)((q.steps + share - 1) / share) : 1;
+    const Request q = base == 0 ? head : request<ROWS, KEYS>(a, base + tid);
+    const int splits = q.steps > share ? 1 + (q.steps - 1) / share : 1;
     const int64_t n = (int64_t)q.tiles * splits, mine = n + (splits > 1 ? n << 32 : 0);
     const int64_t incl = wave_scan(mine);
     if (lane == 63) sums[wave] = incl;
@@ -145,14 +149,68 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int at, Item& it) 
     const int64_t i = at - (before & 0xFFFFFFFF);
     if (i >= 0 && i < n) {
       // a request's longest row tile (the last one, if causal) first
-      found = Item{base + tid, q.tiles - 1 - (int)(i / splits), (int)(i % splits), splits,
+      found = Item{base + tid, q.tiles - 1 - (int)i / splits, (int)i % splits, splits, 0, 0,
                    splits > 1 ? (int)(before >> 32) : -1, q.start, q.fresh, q.kv, min(q.fresh, a.max_new) * a.group};
     }
     __syncthreads();
     if (found.r >= 0) break;
   }
-  it = found;
-  return it.r >= 0;
+  return found.r >= 0;
+}
+
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)v) |
+                   (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)v >> 32)) << 32);
+}
+__device__ __forceinline__ Item uniform(const Item& i) {  // the same for all threads, to the compiler too
+  return Item{__builtin_amdgcn_readfirstlane(i.r), __builtin_amdgcn_readfirstlane(i.tile), __builtin_amdgcn_readfirstlane(i.split),
+              __builtin_amdgcn_readfirstlane(i.splits), __builtin_amdgcn_readfirstlane(i.first), __builtin_amdgcn_readfirstlane(i.last),
+              __builtin_amdgcn_readfirstlane(i.part), __builtin_amdgcn_readfirstlane(i.start), __builtin_amdgcn_readfirstlane(i.fresh),
+              __builtin_amdgcn_readfirstlane(i.kv), __builtin_amdgcn_readfirstlane(i.rows)};
+}
+
+// NARROW: the steps of all heads, requests and row tiles, one after the other, are dealt out evenly: workgroup b of 2^slots takes
+// those from first_step(b) up to first_step(b + 1), one at least if there are so few.
+__device__ __forceinline__ int64_t first_step(int64_t total, int b, int slots) {
+  return total >> slots ? (int64_t)(((unsigned __int128)total * (unsigned)b) >> slots) : min((int64_t)b, total);
+}
+__device__ __forceinline__ int workgroup_of(int64_t total, int64_t step, int slots) {  // the last whose first step is that one or before
+  if (!(total >> slots)) return (int)step;
+  int b = (int)((float)step / (float)total * (float)(1 << slots));
+  b = min(max(b, 0), (1 << slots) - 1);
+  while (first_step(total, b, slots) > step) --b;
+  while (b + 1 < 1 << slots && first_step(total, b + 1, slots) <= step) ++b;
+  return b;
+}
+
+// The request among `from` and the ones behind it that holds step `at`, of which `below` lie before request `from`: its number,
+// lengths and the steps before it, into LDS.  With `heads`, the steps before every request are written there.
+struct Stretch { int64_t below; Request q; int r; };
+template <int ROWS, int KEYS>
+__device__ __forceinline__ void find_request(const PagedArgs& a, int from, int64_t below, int64_t at, int64_t* sums, Stretch& out, int64_t* heads) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (tid == 0) out.r = -1;
+  __syncthreads();
+  for (int base = from; base < a.R; base += THREADS) {
+    const Request q = request<ROWS, KEYS>(a, base + tid);
+    const int64_t n = (int64_t)q.tiles * q.steps, incl = wave_scan(n);
+    if (lane == 63) sums[wave] = incl;
+    __syncthreads();
+    int64_t before = below + incl - n;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) before += sums[w];
+      below += sums[w];
+    }
+    if (heads && base + tid < a.R) heads[base + tid] = before;
+    if (before <= at && at < before + n) {
+      out.below = before;
+      out.q = q;
+      out.r = base + tid;
+    }
+    __syncthreads();
+    if (!heads && out.r >= 0) break;
+  }
 }
 
 // ---- matrix products of a block -----------------------------------------------------------
@@ -165,21 +223,18 @@ __device__ __forceinline__ uint32_t no_numbers(uint32_t w) {
   else return ((w & 0x7F800000u) + 0x00800000u) & 0x80000000u;
 }
 
+// One item: a row tile of a request and a head of keys, and the steps of its keys that are this workgroup's.
 template <typename T, int DB, bool NARROW>
-__global__ __launch_bounds__(THREADS, NARROW || (sizeof(T) == 4 && DB > 2) ? 1 : 2) void paged_attention_kernel(const PagedArgs a) {
+__device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, const int kv_head, unsigned char* const lds) {
   using Sh = Shape<T, DB, NARROW>;
   constexpr bool BF16 = sizeof(T) == 2;
   constexpr int KS = Sh::KS, ROWB = Sh::ROWB;
-  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   typedef typename std::conditional<BF16, bf16x8, f32x4>::type Piece;
 
-  Item it;
-  const int kv_head = blockIdx.x % a.kv_heads;
-  if (!find_item<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, blockIdx.x / a.kv_heads, it)) return;
-  it.r = __builtin_amdgcn_readfirstlane(it.r);
+  const Item it = uniform(found);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 31, g = lane >> 5;
-  if (a.head && tid == 0 && kv_head == 0 && it.tile == 0 && it.split == 0) {
+  if (!NARROW && a.head && tid == 0 && kv_head == 0 && it.tile == 0 && it.split == 0) {
     a.head[2 * it.r] = it.part;
     a.head[2 * it.r + 1] = it.splits;
   }
@@ -194,18 +249,23 @@ __global__ __launch_bounds__(THREADS, NARROW || (sizeof(T) == 4 && DB > 2) ? 1 :
   const int row = min(row0 + lq, it.rows - 1);
   const bool active = __builtin_amdgcn_readfirstlane(row0 < it.rows);
   const int seen = sees(row);
+  const int seen_by_all = __builtin_amdgcn_readfirstlane(sees(min(it.tile * Sh::ITEM_ROWS, it.rows - 1)));  // ... of the workgroup
   const int all_see = __builtin_amdgcn_readfirstlane(sees(min(row0, it.rows - 1)));          // keys that all rows of the wave see
   const int some_see = __builtin_amdgcn_readfirstlane(sees(min(row0 + 31, it.rows - 1)));    // ... that one of them does
   const int tile_sees = __builtin_amdgcn_readfirstlane(sees(min(it.tile * Sh::ITEM_ROWS + Sh::ITEM_ROWS - 1, it.rows - 1)));
   // this workgroup's steps of ITEM_KEYS keys
-  const int steps = (tile_sees + Sh::ITEM_KEYS - 1) / Sh::ITEM_KEYS;
-  const int first = __builtin_amdgcn_readfirstlane((int)((int64_t)steps * it.split / it.splits));
-  const int last = __builtin_amdgcn_readfirstlane((int)((int64_t)steps * (it.split + 1) / it.splits));
-  const int token = row / a.group, head = kv_head * a.group + (row - token * a.group);
+  int first = it.first, last = it.last;
+  if (!NARROW) {
+    const int steps = (tile_sees + Sh::ITEM_KEYS - 1) / Sh::ITEM_KEYS;
+    const int even = steps / it.splits, more = steps - even * it.splits;  // the first `more` parts have a step more
+    first = __builtin_amdgcn_readfirstlane(it.split * even + min(it.split, more));
+    last = __builtin_amdgcn_readfirstlane(first + even + (it.split < more ? 1 : 0));
+  }
 
   Piece qf[KS];
   const int pieces = a.dh * Sh::ES / 16;  // of a head's row
   {
+    const int token = row / a.group, head = kv_head * a.group + (row - token * a.group);
     const T* q = (const T*)a.q + (int64_t)(it.start + token) * a.q_stride + (int64_t)head * a.dh;
     const uint32_t flip = !a.negative ? 0u : BF16 ? 0x80008000u : 0x80000000u;
 #pragma unroll
@@ -224,7 +284,7 @@ __global__ __launch_bounds__(THREADS, NARROW || (sizeof(T) == 4 && DB > 2) ? 1 :
   const bool full = pieces == Sh::CPR;
   const int row_bytes = a.dh * Sh::ES, in_row = lane % Sh::CPR, in_instr = lane / Sh::CPR;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
-  unsigned char* const mine = lds + (NARROW ? wave * Sh::NS * Sh::STAGE : 0);
+  unsigned char* const mine = lds + (NARROW ? wave * Sh::NS * 2 * Sh::TILE : 0);  // K's tiles, then V's
   auto swk = [](int r) __attribute__((always_inline)) { return Sh::CPR == 8 ? (r >> 1) & 7 : r & 15; };
   auto swv = [](int r) __attribute__((always_inline)) { return !BF16 ? (r & 4) << 1 : Sh::CPR == 8 ? (r & 2) << 1 : (r & 3) << 2; };
   const ScalarTable table = (ScalarTable)(uintptr_t)(a.table + (int64_t)it.r * a.table_stride);
@@ -238,26 +298,38 @@ __global__ __launch_bounds__(THREADS, NARROW || (sizeof(T) == 4 && DB > 2) ? 1 :
     for (int i = 0; i < Sh::PAGES; ++i) p.number[i] = table[min((key + 8 * i) >> a.shift, last_entry)];
     return p;
   };
-  auto dma16 = [&](const unsigned char* page, uint32_t off, uint32_t to) __attribute__((always_inline)) {
-    const uint64_t at = (uint64_t)(uintptr_t)page;
-    // (the builtin's result is signed: as a half of an address it must not be extended)
-    const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at) |
-                          (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32;
+  // M0 holds the place in LDS, which the load takes one wait state behind the write at the least; five are what it needs behind
+  // a vector instruction that writes its address (where the compiler has kept scalars in vector registers)
+  auto dma16 = [&](const unsigned char* base, uint32_t off, uint32_t to) __attribute__((always_inline)) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
   };
-  auto load = [&](int step, const Pages& p, int stage) __attribute__((always_inline)) {
+  const uint32_t base = lds0 + (NARROW ? wave * Sh::NS * 2 * Sh::TILE : wave * Sh::LOAD * ROWB);  // of the wave's loads
+  const uint32_t page_bytes = ((uint32_t)row_bytes << a.shift) * (uint32_t)a.kv_heads;  // (at most 4096 x 1024 x 512)
+  const unsigned char* const keys0 = (const unsigned char*)a.kp + (((uint64_t)kv_head << a.shift) * (uint32_t)row_bytes);
+  const int64_t to_values = (const unsigned char*)a.vp - (const unsigned char*)a.kp;
+  // offsets inside the eight rows of a page look-up, the same for every tile
+  uint32_t k_from[Sh::INSTR], v_from[Sh::INSTR];
+#pragma unroll
+  for (int i = 0; i < Sh::INSTR; ++i) {
+    const int r = i * Sh::RPI + in_instr, row = (NARROW ? 0 : wave * Sh::LOAD) + r;
+    k_from[i] = (r & 7) * row_bytes + ((in_row ^ swk(row)) << 4);
+    v_from[i] = (r & 7) * row_bytes + ((in_row ^ swv(row)) << 4);
+  }
+  auto load = [&](auto values_tag, int step, const Pages& p, uint32_t tile) __attribute__((always_inline)) {
+    constexpr bool VALUES = decltype(values_tag)::value;
     const int key = step_key(step);
-    const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + (uint32_t)(mine - lds) + stage * Sh::STAGE + (NARROW ? 0 : wave * Sh::LOAD * ROWB));
     auto group = [&](auto full_tag) __attribute__((always_inline)) {
+      constexpr bool FULL = decltype(full_tag)::value;
 #pragma unroll
       for (int i = 0; i < Sh::INSTR; ++i) {
-        const int r = i * Sh::RPI;  // first row of the instruction
-        const int number = p.number[r / 8];
-        const int64_t at = ((((int64_t)((unsigned)number < (unsigned)a.n_pages ? number : 0) * a.kv_heads + kv_head) << a.shift) +
-                            ((key + r) & ((1 << a.shift) - 1))) * row_bytes;
-        const int row_in = (NARROW ? 0 : wave * Sh::LOAD) + r + in_instr, ck = in_row ^ swk(row_in), cv = in_row ^ swv(row_in);
-        if (decltype(full_tag)::value || ck < pieces) dma16((const unsigned char*)a.kp + at, in_instr * row_bytes + ck * 16, to + r * ROWB);
-        if (decltype(full_tag)::value || cv < pieces) dma16((const unsigned char*)a.vp + at, in_instr * row_bytes + cv * 16, to + Sh::KEYS * ROWB + r * ROWB);
+        const int eight = i * Sh::RPI / 8;
+        const uint32_t number = (unsigned)p.number[eight] < (unsigned)a.n_pages ? p.number[eight] : 0;
+        const unsigned char* const from = keys0 + (uint64_t)number * page_bytes + (uint32_t)((key + 8 * eight) & ((1 << a.shift) - 1)) * (uint32_t)row_bytes;
+        const uint32_t to = base + tile + i * 1024;
+        int piece = in_row, at = in_instr;
+        if (!FULL) asm("" : "+v"(piece), "+v"(at));  // compared again every time: kept, the lanes' masks are more scalars than there are
+        const int row = (NARROW ? 0 : wave * Sh::LOAD) + i * Sh::RPI + at;
+        if (FULL || (piece ^ (VALUES ? swv(row) : swk(row))) < pieces) dma16(VALUES ? from + to_values : from, VALUES ? v_from[i] : k_from[i], to);
       }
     };
     if (full) group(std::true_type{});
@@ -283,15 +355,21 @@ __global__ __launch_bounds__(THREADS, NARROW || (sizeof(T) == 4 && DB > 2) ? 1 :
   // In bf16 the sums of the weights come from two small products with ones: column n of a 16 x 16 x 32 product sums the eight
   // values of the lanes n, n + 16, n + 32 and n + 48, of the rows n and n + 16 that is; a first operand with ones for the
   // lanes of one in its even rows and for those of the other in its odd rows tells them apart.
-  bf16x8 ones;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) ones[e] = (__bf16)(((lane ^ (lane >> 4)) & 1) ? 0.0f : 1.0f);
-  const uint32_t k_off = (uint32_t)(lq * ROWB + ((g ^ swk(lq)) << 4));
+  const uint32_t two_ones = ((lane ^ (lane >> 4)) & 1) ? 0u : 0x3F803F80u;
+  uint32_t k_off = (uint32_t)(lq * ROWB + ((g ^ swk(lq)) << 4));
   // (the transposing read: lane j of 16 points at four columns of key j / 4 and receives column j of the four keys)
   const uint32_t v_row = BF16 ? 4 * g + ((lane & 15) >> 2) : 4 * g;
-  const uint32_t v_off = BF16 ? v_row * ROWB + 32 * ((lane >> 4) & 1) + 8 * (lane & 3) : v_row * ROWB + (lq & 3) * 4;
-  const uint32_t v_swap = BF16 ? (Sh::CPR == 8 ? (lane & 8) << 3 : ((lane & 15) >> 2) << 6) : 0;
+  uint32_t v_off = BF16 ? v_row * ROWB + 32 * ((lane >> 4) & 1) + 8 * (lane & 3) : v_row * ROWB + (lq & 3) * 4;
+  uint32_t v_swap = BF16 ? (Sh::CPR == 8 ? (lane & 8) << 3 : ((lane & 15) >> 2) << 6) : 0;
   auto read_k = [&](const unsigned char* sK, int ks) __attribute__((always_inline)) { return *(const Piece*)(sK + (k_off ^ (uint32_t)(ks << 5))); };
+  auto first_product = [&](f32x16& st, const Piece& k, int ks) __attribute__((always_inline)) {
+    if constexpr (BF16) {
+      st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qf[ks], st, 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) st = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], qf[ks][e], st, 0, 0, 0);
+    }
+  };
   auto read_v16 = [&](const unsigned char* sV, int b, int s2) __attribute__((always_inline)) {  // bf16: keys 16 s2 + 4 g + (0 .. 3, 8 .. 11), column 32 b + lq
     const unsigned char* p = sV + s2 * 16 * ROWB + ((uint32_t)(b * 64) ^ v_swap) + v_off;
     const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p));
@@ -322,7 +400,7 @@ __global__ __launch_bounds__(THREADS, NARROW || (sizeof(T) == 4 && DB > 2) ? 1 :
   // (counted by a product of ones) get what it makes of a sum.
   auto any_no_number = [&](const unsigned char* sV) __attribute__((always_inline)) {
     uint32_t any = 0;
-#pragma unroll
+#pragma unroll 1
     for (int b = 0; b < DB; ++b) {
       if constexpr (BF16) {
 #pragma unroll
@@ -382,36 +460,47 @@ __global__ __launch_bounds__(THREADS, NARROW || (sizeof(T) == 4 && DB > 2) ? 1 :
     }
   };
 
-  // FAST: weights exp2(x - m) with the maximum m of the row's first block for all of its keys, which serves any row whose sum of
-  // weights stays between 2^-100 and 2^100 (bf16 and fp32 have the same exponents, so nothing is lost); a wave with another row goes over its keys again with a running maximum.
-  bool begun = false;
-  auto block = [&](auto fast_tag, auto mask_tag, const unsigned char* sK, const unsigned char* sV, int key0, uint32_t bad) __attribute__((always_inline)) {
-    constexpr bool FAST = decltype(fast_tag)::value, MASK = decltype(mask_tag)::value;
+  // Weights are exp2(x - m) with the maximum m of the row's first block for all of its keys, which serves any row whose sum of
+  // weights stays between 2^-100 and 2^100 (bf16 and fp32 have the same exponents, so nothing is lost); a wave with another
+  // row goes over its keys again with a running maximum (`fast` is false then).
+  bool fast = true, begun = false;
+  float neg_m = 0.f;
+  auto logits = [&](const unsigned char* sK) __attribute__((always_inline)) {
     f32x16 st;
 #pragma unroll
     for (int v = 0; v < 16; ++v) st[v] = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const Piece k = read_k(sK, ks);
-      if constexpr (BF16) {
-        st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qf[ks], st, 0, 0, 0);
-      } else {
+    for (int ks = 0; ks < KS; ++ks) first_product(st, read_k(sK, ks), ks);
+    return st;
+  };
+  auto weight = [&](float x) __attribute__((always_inline)) { return __builtin_amdgcn_exp2f(fmaf(x, a.scale, neg_m)); };
+  auto sum_ones = [&](const uint32_t (&pw)[8]) __attribute__((always_inline)) {
+    uint32_t w = two_ones;
+    asm("" : "+v"(w));  // one register between two blocks, not four
+    const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{w, w, w, w});
 #pragma unroll
-        for (int e = 0; e < 4; ++e) st = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], qf[ks][e], st, 0, 0, 0);
-      }
-    }
+    for (int s2 = 0; s2 < 2; ++s2)
+      lsum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, u32x4{pw[4 * s2], pw[4 * s2 + 1], pw[4 * s2 + 2], pw[4 * s2 + 3]}),
+                                                     lsum, 0, 0, 0);
+  };
+  auto block = [&](auto mask_tag, const unsigned char* sK, const unsigned char* sV, int key0, uint32_t bad) __attribute__((always_inline)) {
+    constexpr bool MASK = decltype(mask_tag)::value;
+    // the general block works its places in LDS out again: kept for it, they would be registers that the others have not got
+    const uint32_t keep[3] = {k_off, v_off, v_swap};
+    if (MASK) asm("" : "+v"(k_off), "+v"(v_off), "+v"(v_swap));
+    f32x16 st = logits(sK);
     if (MASK) {
 #pragma unroll
       for (int v = 0; v < 16; ++v)
         if (key0 + 8 * (v >> 2) + 4 * g + (v & 3) >= seen || (bad >> (v >> 2) & 1)) st[v] = -INFINITY;
     }
-    if (!FAST || !begun) {
+    if (MASK && (!begun || !fast)) {
       float up = st[0];
 #pragma unroll
       for (int v = 1; v < 16; ++v) up = fmaxf(up, st[v]);
       up = fmaxf(up, __shfl_xor(up, 32, 64)) * a.scale;
       up = fmaxf(up, m);
-      if (!FAST) {
+      if (begun) {
         const float shrink = up == m ? 1.f : __builtin_amdgcn_exp2f(m - up);
         l *= shrink;
 #pragma unroll
@@ -421,36 +510,36 @@ __global__ __launch_bounds__(THREADS, NARROW || (sizeof(T) == 4 && DB > 2) ? 1 :
       }
       m = up;
       begun = true;
+      neg_m = m == -INFINITY ? 0.f : -m;
     }
-    const float neg_m = m == -INFINITY ? 0.f : -m;
     uint32_t pw[8];
     f32x16 pf;
-    float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float x = __builtin_amdgcn_exp2f(fmaf(st[2 * e], a.scale, neg_m)), y = __builtin_amdgcn_exp2f(fmaf(st[2 * e + 1], a.scale, neg_m));
+      const float x = weight(st[2 * e]), y = weight(st[2 * e + 1]);
       if constexpr (BF16) {
         pw[e] = pack_bf16x2(x, y);
-        if (!FAST) sum += __builtin_bit_cast(float, pw[e] << 16) + __builtin_bit_cast(float, pw[e] & 0xFFFF0000u);
+        if (MASK && !fast) l += __builtin_bit_cast(float, pw[e] << 16) + __builtin_bit_cast(float, pw[e] & 0xFFFF0000u);
       } else {
         pf[2 * e] = x;
         pf[2 * e + 1] = y;
-        sum += x + y;
+        l += x + y;
       }
     }
-    if constexpr (FAST && BF16) {
-#pragma unroll
-      for (int s2 = 0; s2 < 2; ++s2)
-        lsum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, u32x4{pw[4 * s2], pw[4 * s2 + 1], pw[4 * s2 + 2], pw[4 * s2 + 3]}),
-                                                       lsum, 0, 0, 0);
-    } else {
-      l += sum;
-    }
+    if (BF16 && (!MASK || fast)) sum_ones(pw);
     if (MASK && any_no_number(sV)) accumulate_around(sV, pw, pf, st);
     else accumulate(sV, pw, pf);
+    k_off = keep[0];
+    v_off = keep[1];
+    v_swap = keep[2];
   };
   const std::true_type YES{};
   const std::false_type NO{};
+  // a block at key0, of which the wave's rows see all, some or none
+  auto any_block = [&](const unsigned char* sK, const unsigned char* sV, int key0, uint32_t bad) __attribute__((always_inline)) {
+    if (fast && begun && key0 + 32 <= all_see && !bad) block(NO, sK, sV, key0, 0);
+    else if (key0 < some_see) block(YES, sK, sV, key0, bad);
+  };
 
   auto clear = [&]() __attribute__((always_inline)) {
     m = -INFINITY;
@@ -462,60 +551,154 @@ __global__ __launch_bounds__(THREADS, NARROW || (sizeof(T) == 4 && DB > 2) ? 1 :
 #pragma unroll
       for (int v = 0; v < 16; ++v) o[b][v] = 0.f;
   };
-  auto finish = [&](auto fast_tag) __attribute__((always_inline)) {  // the whole sum of a row, in both lanes that share it
-    if constexpr (decltype(fast_tag)::value && BF16) l = lane & 16 ? lsum[1] : lsum[0];
+  auto finish = [&]() __attribute__((always_inline)) {  // the whole sum of a row, in both lanes that share it
+    int upper = lane & 16;
+    asm("" : "+v"(upper));
+    if (BF16 && fast) l = upper ? lsum[1] : lsum[0];
     else l += __shfl_xor(l, 32, 64);
   };
   auto wait = []() __attribute__((always_inline)) { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
 
-  // WIDE: a tile is loaded while the one before it is worked on; one barrier a tile, behind which the tile is complete and
-  // nobody reads the buffer that the next loads fill.
+  // WIDE: tiles that all rows see are worked on in pairs without branches.  A block's logits are formed while the exponentials of
+  // the one before are, one or a few behind each matrix instruction, and every fragment is read a product ahead of its use.  A
+  // tile's K is read for the last time a tile ahead of its V, so K's loads run a tile ahead of V's and one barrier a tile
+  // does: behind it K of the next tile and V of this one are complete, and nobody reads the buffers that the next loads fill.
   bool careful = false;  // a page of the workgroup's keys lies outside the pool
-  auto wide_pass = [&](auto fast_tag, const bool work) __attribute__((always_inline)) {
-    if (work) clear();
-    Pages next = look_up(first);
-    load(first, next, first & 1);
-    next = look_up(first + 1);
-    for (int t = first; t < last; ++t) {
+  auto hot_block = [&](Piece (&kf)[KS], const unsigned char* sV, const unsigned char* next_k, f32x16& now, f32x16& next) __attribute__((always_inline)) {
+    bf16x8 vf[DB][2];
+    if constexpr (BF16) {
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2) vf[b][s2] = read_v16(sV, b, s2);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    uint32_t pw[8];
+    f32x16 pf;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) next[v] = 0.f;
+    // behind each matrix instruction the arguments of a pair of weights, the exponentials of the pair before and the rounding of
+    // the one before that: nothing waits for what was issued just ahead of it
+    auto pair = [&](int e) __attribute__((always_inline)) {
+      if (e < 8) {
+        now[2 * e] = fmaf(now[2 * e], a.scale, neg_m);
+        now[2 * e + 1] = fmaf(now[2 * e + 1], a.scale, neg_m);
+      }
+      if (e >= 1 && e < 9) {
+        pf[2 * e - 2] = __builtin_amdgcn_exp2f(now[2 * e - 2]);
+        pf[2 * e - 1] = __builtin_amdgcn_exp2f(now[2 * e - 1]);
+      }
+      if (e >= 2) {
+        if constexpr (BF16) pw[e - 2] = pack_bf16x2(pf[2 * e - 4], pf[2 * e - 3]);
+        else l += pf[2 * e - 4] + pf[2 * e - 3];
+      }
+    };
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      first_product(next, kf[ks], ks);
+#pragma unroll
+      for (int e = 10 * ks / KS; e < 10 * (ks + 1) / KS; ++e) pair(e);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) kf[ks] = read_k(next_k, ks);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (BF16) {
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2)
+          o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[b][s2], __builtin_bit_cast(bf16x8, u32x4{pw[4 * s2], pw[4 * s2 + 1], pw[4 * s2 + 2], pw[4 * s2 + 3]}), o[b], 0, 0, 0);
+      sum_ones(pw);
+    } else {
+      accumulate(sV, pw, pf);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto wide_pass = [&](const bool work) __attribute__((always_inline)) {
+    auto k_at = [](int t) __attribute__((always_inline)) { return (t & 1) * Sh::TILE; };
+    auto v_at = [](int t) __attribute__((always_inline)) { return (2 + (t & 1)) * Sh::TILE; };
+    Pages p1 = look_up(first);
+    load(NO, first, p1, k_at(first));
+    load(YES, first, p1, v_at(first));
+    p1 = look_up(first + 1);  // of the tile behind the present one, and of the one behind that
+    if (first + 1 < last) load(NO, first + 1, p1, k_at(first + 1));
+    Pages p2{};
+    auto enter = [&](int t) __attribute__((always_inline)) {
+      // (scalar loads come in any order: with one on its way, whoever waits for LDS waits for all of it.  The barrier does so anyway.)
+      p2 = look_up(t + 2);
       wait();
       __syncthreads();
-      if (t + 1 < last) {
-        load(t + 1, next, (t + 1) & 1);
-        next = look_up(t + 2);
-      }
-      if (!work) continue;
-      const unsigned char* sK = lds + (t & 1) * Sh::STAGE;
-      const unsigned char* sV = sK + Sh::KEYS * ROWB;
-#pragma unroll
-      for (int kb = 0; kb < Sh::KEYS / 32; ++kb) {
-        const int key0 = t * Sh::ITEM_KEYS + kb * 32;
-        if (key0 + 32 <= all_see && !careful) {
-          block(fast_tag, NO, sK + kb * 32 * ROWB, sV + kb * 32 * ROWB, key0, 0);
-        } else if (key0 < some_see) {
+      if (t + 1 < last) load(YES, t + 1, p1, v_at(t + 1));
+    };
+    auto further = [&](int t) __attribute__((always_inline)) {
+      if (t + 2 < last) load(NO, t + 2, p2, k_at(t));
+      p1 = p2;
+    };
+    if (work) clear();
+    const int hot_end = fast && !careful ? min(last, seen_by_all / Sh::ITEM_KEYS) : 0;
+    int t = first;
+#pragma unroll 1
+    do {
+      enter(t);
+      if (work) {
+#pragma unroll 1
+        for (int kb = 0; kb < 2; ++kb) {
+          const int key0 = t * Sh::ITEM_KEYS + kb * 32;
           uint32_t bad = 0;
           if (careful) {
             for (int i = 0; i < 4; ++i)
               bad |= (unsigned)table[min((key0 + 8 * i) >> a.shift, last_entry)] < (unsigned)a.n_pages ? 0u : 1u << i;
           }
-          block(fast_tag, YES, sK + kb * 32 * ROWB, sV + kb * 32 * ROWB, key0, bad);
+          if (key0 < some_see) block(YES, lds + k_at(t) + kb * 32 * ROWB, lds + v_at(t) + kb * 32 * ROWB, key0, bad);
         }
       }
-    }
-    if (work) finish(fast_tag);
+      __syncthreads();
+      further(t);
+      ++t;
+      if ((t & 1) || t + 1 >= hot_end) continue;
+      if (work) {
+        Piece kf[KS];
+        f32x16 s0 = logits(lds), s1;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kf[ks] = read_k(lds + 32 * ROWB, ks);
+#pragma unroll 1
+        for (; t + 1 < hot_end; t += 2) {
+          enter(t);
+          further(t);
+          hot_block(kf, lds + 2 * Sh::TILE, lds + Sh::TILE, s0, s1);
+          hot_block(kf, lds + 2 * Sh::TILE + 32 * ROWB, lds + Sh::TILE + 32 * ROWB, s1, s0);
+          enter(t + 1);
+          further(t + 1);
+          hot_block(kf, lds + 3 * Sh::TILE, lds, s0, s1);
+          hot_block(kf, lds + 3 * Sh::TILE + 32 * ROWB, lds + 32 * ROWB, s1, s0);
+        }
+      } else {
+#pragma unroll 1
+        for (; t + 1 < hot_end; t += 2) {  // (as many barriers)
+          enter(t);
+          further(t);
+          enter(t + 1);
+          further(t + 1);
+        }
+      }
+    } while (t < last);
+    if (work) finish();
     __syncthreads();  // before the buffers are used again
   };
   // NARROW: a wave waits for its own loads alone, of which a stage more is on its way.
-  auto narrow_pass = [&](auto fast_tag) __attribute__((always_inline)) {
+  auto narrow_pass = [&]() __attribute__((always_inline)) {
     clear();
     constexpr int LOADS = 2 * Sh::INSTR;
     uint32_t bad[2] = {0u, 0u};
+    auto load_both = [&](int t, const Pages& p, int s) __attribute__((always_inline)) {
+      bad[s] = bad_pages(p);
+      load(NO, t, p, s * 2 * Sh::TILE);
+      load(YES, t, p, (s * 2 + 1) * Sh::TILE);
+    };
 #pragma unroll
     for (int s = 0; s < Sh::NS; ++s)
-      if (first + s < last) {
-        const Pages p = look_up(first + s);
-        bad[s] = bad_pages(p);
-        load(first + s, p, s);
-      }
+      if (first + s < last) load_both(first + s, look_up(first + s), s);
     for (int t0 = first; t0 < last; t0 += Sh::NS) {
 #pragma unroll
       for (int s = 0; s < Sh::NS; ++s) {
@@ -525,19 +708,14 @@ __global__ __launch_bounds__(THREADS, NARROW || (sizeof(T) == 4 && DB > 2) ? 1 :
         if (t + Sh::NS < last) p = look_up(t + Sh::NS);
         if (Sh::NS > 1 && t + 1 < last) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
         else wait();
-        const unsigned char* sK = mine + s * Sh::STAGE;
-        const unsigned char* sV = sK + Sh::KEYS * ROWB;
-        const int key0 = step_key(t);
-        if (key0 + 32 <= all_see && !bad[s]) block(fast_tag, NO, sK, sV, key0, 0);
-        else if (key0 < some_see) block(fast_tag, YES, sK, sV, key0, bad[s]);
+        any_block(mine + s * 2 * Sh::TILE, mine + (s * 2 + 1) * Sh::TILE, step_key(t), bad[s]);
         if (t + Sh::NS < last) {
-          bad[s] = bad_pages(p);
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the block's reads of this stage are through
-          load(t + Sh::NS, p, s);
+          load_both(t + Sh::NS, p, s);
         }
       }
     }
-    finish(fast_tag);
+    finish();
   };
 
   // a row that sees keys of this part and whose sum is out of range
@@ -546,31 +724,48 @@ __global__ __launch_bounds__(THREADS, NARROW || (sizeof(T) == 4 && DB > 2) ? 1 :
     return __builtin_amdgcn_ballot_w64(sees_some && !(l >= 0x1p-100f && l <= 0x1p100f)) != 0;
   };
   if constexpr (NARROW) {
-    narrow_pass(YES);
-    if (out_of_range()) narrow_pass(NO);
+    if (all == 0) {
+      clear();
+    } else {
+#pragma unroll 1
+      for (;;) {
+        narrow_pass();
+        if (!fast || !out_of_range()) break;
+        fast = false;
+      }
+    }
   } else if (first < last) {
     bool bad = false;
     for (int i = ((first * Sh::ITEM_KEYS) >> a.shift) + tid; i <= min((last * Sh::ITEM_KEYS - 1) >> a.shift, last_entry); i += THREADS)
       bad |= (unsigned)a.table[(int64_t)it.r * a.table_stride + i] >= (unsigned)a.n_pages;
     careful = __syncthreads_or(bad);
-    wide_pass(YES, active);
-    // rows of a wave that was in range stay as they are, whatever shares their workgroup
-    const bool again = active && out_of_range();
-    if (__syncthreads_or(again)) wide_pass(NO, again);
+    bool work = active;
+#pragma unroll 1
+    for (;;) {
+      wide_pass(work);
+      // rows of a wave that was in range stay as they are, whatever shares their workgroup
+      work = work && out_of_range();
+      if (!fast || !__syncthreads_or(work)) break;
+      fast = false;
+    }
   } else {
     clear();
   }
 
   // ---- results: a lane owns a row; registers 4 j .. 4 j + 3 of block b are its columns 32 b + 8 j + 4 g .. + 3
-  const int64_t part = it.part >= 0 ? ((int64_t)it.part + (int64_t)it.tile * it.splits + it.split) * a.kv_heads + kv_head : -1;
+  const Item in = uniform(found);  // (read again: kept through the loops, it would be registers that they have not got)
+  const int64_t part = NARROW ? in.part : in.part >= 0 ? ((int64_t)in.part + (int64_t)in.tile * in.splits + in.split) * a.kv_heads + kv_head : -1;
   if (part >= a.max_parts) return;  // (only if the offsets are none: requests that overlap)
   auto store = [&](int col, f32x4 v, int64_t at) __attribute__((always_inline)) {  // four columns of the row at element `at` of out
     if constexpr (BF16) *(u32x2*)((bf16_t*)a.out + at + col) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
     else *(f32x4*)((float*)a.out + at + col) = v;
   };
   if constexpr (!NARROW) {
-    if (!active || row0 + lq >= it.rows) return;
-    const int64_t at = (int64_t)(it.start + token) * a.out_stride + (int64_t)head * a.dh;
+    int own_row = row0 + lq;
+    asm("" : "+v"(own_row));  // (worked out here, not ahead of the loops)
+    if (!active || own_row >= in.rows) return;
+    const int token = own_row / a.group, head = kv_head * a.group + (own_row - token * a.group);
+    const int64_t at = (int64_t)(in.start + token) * a.out_stride + (int64_t)head * a.dh;
     const float inv = part >= 0 ? 1.f : l == 0.f ? 0.f : 1.f / l;
     float* const po = a.parts + (part * a.part_rows + wave * 32 + lq) * (DB * 32);
     if (part >= 0 && g == 0) {
@@ -592,7 +787,7 @@ __global__ __launch_bounds__(THREADS, NARROW || (sizeof(T) == 4 && DB > 2) ? 1 :
     float* const ms = (float*)lds;              // [4][32] maxima, [4][32] sums
     float* const so = (float*)(lds + 1024);     // [4][32][32 DB + 4]: rows a bank apart
     constexpr int LD = DB * 32 + 4;
-    const int rows = min(32, it.rows - row0);
+    const int rows = min(32, in.rows - row0);
     if (g == 0) {
       ms[wave * 32 + lq] = m;
       ms[128 + wave * 32 + lq] = l;
@@ -632,73 +827,182 @@ __global__ __launch_bounds__(THREADS, NARROW || (sizeof(T) == 4 && DB > 2) ? 1 :
         }
       } else if (col < a.dh) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        store(col, f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv}, (int64_t)(it.start + tok) * a.out_stride + (int64_t)hd * a.dh);
+        store(col, f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv}, (int64_t)(in.start + tok) * a.out_stride + (int64_t)hd * a.dh);
       }
     }
   }
 }
 
-// A wave for every row of a request whose keys were divided: its parts, in order.
-template <typename T, int DB>
-__global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a, int item_rows) {
-  const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
+template <typename T, int DB, bool NARROW>
+__global__ __launch_bounds__(THREADS, (NARROW || sizeof(T) == 4) && DB > 2 ? 1 : 2) void paged_attention_kernel(const PagedArgs a) {
+  using Sh = Shape<T, DB, NARROW>;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  __shared__ Item found;
+  if constexpr (!NARROW) {
+    if (!find_item<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, blockIdx.x / a.kv_heads, found)) return;
+    work_on<T, DB, NARROW>(a, found, blockIdx.x % a.kv_heads, lds);
+  } else {
+    __shared__ int64_t sums[4];
+    __shared__ Stretch stretch;
+    const int tid = threadIdx.x;
+    int64_t steps = 0;  // of a head of keys
+    for (int r = tid; r < a.R; r += THREADS) {
+      const Request q = request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, r);
+      steps += (int64_t)q.tiles * q.steps;
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) steps += __shfl_xor(steps, d, 64);
+    if ((tid & 63) == 0) sums[tid >> 6] = steps;
+    __syncthreads();
+    steps = uniform(sums[0] + sums[1] + sums[2] + sums[3]);
+    __syncthreads();
+    const int64_t total = steps * a.kv_heads, from = first_step(total, blockIdx.x, a.slots), to = first_step(total, blockIdx.x + 1, a.slots);
+    int64_t* const heads = blockIdx.x == 0 ? (int64_t*)a.head : nullptr;
+    if (heads) {
+      if (tid == 0) heads[0] = steps;
+      find_request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, 0, 0, -1, sums, stretch, heads + 1);
+    }
+    int kv_head = 0, r = 0;
+    int64_t below = 0, at = from;
+    if (from < to) {
+      kv_head = (int)(from / steps);
+      at = from - kv_head * steps;
+    }
+#pragma unroll 1
+    for (int64_t done = from; done < to;) {
+      find_request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, r, below, at, sums, stretch, nullptr);
+      r = __builtin_amdgcn_readfirstlane(stretch.r);
+      if (r < 0) return;  // (only if the lengths have changed meanwhile)
+      below = uniform(stretch.below);
+      const Request q = stretch.q;
+      const int tiles = __builtin_amdgcn_readfirstlane(q.tiles), its = __builtin_amdgcn_readfirstlane(q.steps);
+      int tile = (int)((at - below) / its), first = (int)(at - below - (int64_t)tile * its);
+#pragma unroll 1
+      for (; tile < tiles && done < to; ++tile, first = 0) {
+        const int last = (int)min((int64_t)its, first + (to - done));
+        if (tid == 0) {
+          // a workgroup leaves a part of its first item and one of its last at the most
+          const int part = first == 0 && last == its ? -1 : 2 * (int)blockIdx.x + (done == from ? 0 : 1);
+          found = Item{r, tile, 0, 1, first, last, part, q.start, q.fresh, q.kv, min(q.fresh, a.max_new) * a.group};
+        }
+        __syncthreads();
+        work_on<T, DB, NARROW>(a, found, kv_head, lds);
+        __syncthreads();  // before LDS is used again
+        done += last - first;
+        at += last - first;
+      }
+      below += (int64_t)tiles * its;
+      ++r;
+      if (at == steps) {
+        ++kv_head;
+        at = below = 0;
+        r = 0;
+      }
+    }
+  }
+}
+
+// The parts of a row whose request's keys were divided, in order.  Half a wave takes a part, 16 bytes a lane, four parts at a time: the
+// loads' latencies are what this kernel is.  HALVES of them share a row: one where rows are many, all eight of a
+// workgroup where they are few and may have many parts each.
+template <typename T, int DB, bool NARROW, int HALVES>
+__global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
+  using Sh = Shape<T, DB, NARROW>;
+  const int half = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t i = HALVES == 1 ? (int64_t)blockIdx.x * 8 + half : blockIdx.x;
   const int t = (int)(i / a.heads), head = (int)(i - (int64_t)t * a.heads);
   if (t >= a.rows) return;
-  int lo = 0, hi = a.R;  // requests lo .. hi - 1 hold the one that starts at t or below last
+  int lo = 0, hi = a.R;  // of the requests lo .. hi - 1 one is the last to start at t or below
   while (hi - lo > 1) {
-    const int step = (hi - lo + 63) / 64, at = lo + lane * step;
-    const int n = __popcll(__builtin_amdgcn_ballot_w64(at < hi && a.starts[min(at, hi - 1)] <= t));
+    const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+    const uint64_t some = __builtin_amdgcn_ballot_w64(at < hi && a.starts[min(at, hi - 1)] <= t);
+    const int n = __popc((uint32_t)(some >> (threadIdx.x & 32)));
     if (n == 0) return;
     lo += (n - 1) * step;
     hi = min(hi, lo + step);
   }
   const int start = a.starts[lo], fresh = a.starts[lo + 1] - start;
   if (t < start || t - start >= min(fresh, a.max_new)) return;
-  const int first = a.head[2 * lo], splits = a.head[2 * lo + 1];
-  if (first < 0) return;
   const int kv_head = head / a.group, row = (t - start) * a.group + (head - kv_head * a.group);
-  const int tile = row / item_rows, in_tile = row - tile * item_rows;
-  // the places of its parts lie kv_heads parts apart
-  const int64_t part = ((int64_t)first + (int64_t)tile * splits) * a.kv_heads + kv_head;
-  if (splits < 1 || part + (int64_t)(splits - 1) * a.kv_heads >= a.max_parts) return;  // (as above: nobody has written it)
-  const float* const stats = a.stats + (part * a.part_rows + in_tile) * 2;
-  const int64_t stats_step = (int64_t)a.kv_heads * a.part_rows * 2, step = (int64_t)a.kv_heads * a.part_rows * (DB * 32);
-  float top = -INFINITY;
-  for (int s = lane; s < splits; s += 64)
-    if (stats[s * stats_step + 1] != 0.f) top = fmaxf(top, stats[s * stats_step]);
-#pragma unroll
-  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-  const float ref = top == -INFINITY ? 0.f : top;
-  const float* const values = a.parts + (part * a.part_rows + in_tile) * (DB * 32);
-  float sum = 0.f, v[2] = {0.f, 0.f};
-  for (int s0 = 0; s0 < splits; s0 += 64) {
-    float f = 0.f, w = 0.f;
-    if (s0 + lane < splits) {
-      const float l = stats[(s0 + lane) * stats_step + 1], ml = stats[(s0 + lane) * stats_step];
-      if (l != 0.f) f = __builtin_amdgcn_exp2f((ml == -INFINITY ? 0.f : ml) - ref);
-      w = l;
-    }
-    for (int s = 0; s < min(64, splits - s0); ++s) {
-      const float fs = __shfl(f, s, 64), ws = __shfl(w, s, 64);
-      if (ws == 0.f) continue;
-      sum = fmaf(ws, fs, sum);
-      const float* p = values + (s0 + s) * step;
-      if (lane < DB * 32) v[0] = fmaf(p[lane], fs, v[0]);
-      if (lane + 64 < DB * 32) v[1] = fmaf(p[lane + 64], fs, v[1]);
-    }
+  const int tile = row / Sh::ITEM_ROWS, in_tile = row - tile * Sh::ITEM_ROWS;
+  int64_t part, next;  // the row's first part, and how far it is from the second one to the third
+  int64_t second = 0;  // ... and to the second
+  int splits;
+  if constexpr (NARROW) {
+    const int64_t* const heads = (const int64_t*)a.head;
+    const int64_t steps = heads[0];
+    const int its = request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, lo).steps;
+    const int64_t total = steps * a.kv_heads, at = kv_head * steps + heads[1 + lo] + (int64_t)tile * its;
+    const int b0 = workgroup_of(total, at, a.slots), b1 = workgroup_of(total, at + its - 1, a.slots);
+    splits = b1 - b0 + 1;
+    if (splits < 2) return;
+    part = 2 * b0 + (first_step(total, b0, a.slots) == at ? 0 : 1);
+    second = 2 * (b0 + 1) - part;
+    next = 2;
+  } else {
+    const int first = a.head[2 * lo];
+    splits = a.head[2 * lo + 1];
+    if (first < 0) return;
+    part = ((int64_t)first + (int64_t)tile * splits) * a.kv_heads + kv_head;  // the others lie kv_heads parts apart
+    second = next = a.kv_heads;
   }
-  T* out = (T*)a.out + (int64_t)t * a.out_stride + (int64_t)head * a.dh;
+  if (splits < 1 || part < 0 || part + second + (int64_t)(splits - 1) * next >= a.max_parts + next) return;  // (offsets that are none: nobody has written it)
+  const float* const stats = a.stats + (part * a.part_rows + in_tile) * 2;
+  const int64_t one_stats = (int64_t)a.part_rows * 2, one = (int64_t)a.part_rows * (DB * 32);
+  const int col = lane * 4;
+  const float* const values = a.parts + (part * a.part_rows + in_tile) * (DB * 32) + (col < DB * 32 ? col : 0);
+  // a running maximum, as in the parts themselves
+  float top = -INFINITY, sum = 0.f;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](float top2, float sum2, f32x4 v2) __attribute__((always_inline)) {
+    if (sum2 == 0.f) return;  // it saw nothing
+    const float ref = top2 == -INFINITY ? 0.f : top2, up = fmaxf(top, ref);
+    const float keep = __builtin_amdgcn_exp2f(top - up), f = __builtin_amdgcn_exp2f(ref - up);
+    top = up;
+    sum = fmaf(sum2, f, sum * keep);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = fmaf(v2[e], f, v[e] * keep);
+  };
+  for (int s0 = HALVES == 1 ? 0 : half; s0 < splits; s0 += 4 * HALVES) {
+    f32x2 st[4];
+    f32x4 x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int s = min(s0 + u * HALVES, splits - 1);
+      const int64_t from = s == 0 ? 0 : second + (s - 1) * next;
+      st[u] = *(const f32x2*)(stats + from * one_stats);
+      x[u] = *(const f32x4*)(values + from * one);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (s0 + u * HALVES < splits) add(st[u][0], st[u][1], x[u]);
+  }
+  if constexpr (HALVES > 1) {
+    __shared__ float tops[8], sums[8];
+    __shared__ f32x4 all[8][32];
+    if (lane == 0) {
+      tops[half] = top;
+      sums[half] = sum;
+    }
+    all[half][lane] = v;
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+#pragma unroll
+    for (int h = 1; h < 8; ++h) add(tops[h], sums[h], all[h][lane]);
+  }
+  if (col >= a.dh) return;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  if (lane < a.dh) Elem<T>::store(out + lane, v[0] * inv);
-  if (lane + 64 < a.dh) Elem<T>::store(out + lane + 64, v[1] * inv);
+  const int64_t at = (int64_t)t * a.out_stride + (int64_t)head * a.dh + col;
+  if constexpr (sizeof(T) == 2) *(u32x2*)((bf16_t*)a.out + at) = u32x2{pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv)};
+  else *(f32x4*)((float*)a.out + at) = f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
 }
 
 // ---- host ---------------------------------------------------------------------------------
 // How a call is laid out: by the sizes that the host knows, upper bounds of what the device finds.
 struct Layout {
   bool narrow;
-  int target, part_rows, width;   // see PagedArgs; columns of a part's rows
+  bool divide;
+  int slots, part_rows, width;   // see PagedArgs; columns of a part's rows
   int64_t grid, parts;
   size_t head_bytes, stats_bytes, bytes;
 };
@@ -709,20 +1013,20 @@ Layout lay_out(const vit_pages_attend_t* p) {
   Layout y{};
   const int group = p->q_heads / p->kv_heads;
   const int64_t most = (int64_t)p->max_new * group;  // rows of a request and head of keys
-  y.narrow = most <= 32;
+  y.narrow = most <= (p->dtype == VIT_DTYPE_FP32 ? 512 : 32);
   const int rows = y.narrow ? 32 : 128;
   const int64_t tiles = p->kv_heads * std::min<int64_t>((most + rows - 1) / rows * p->n_requests, (int64_t)p->n_rows * group / rows + p->n_requests);
-  y.target = 2 * UNITS;
-  // with rows for several rounds of the device there is nothing to divide
-  if ((int64_t)p->n_rows * group / rows * p->kv_heads >= 4 * y.target || p->table_width == 0) y.target = 0;
+  y.slots = (p->head_dim > 64 && (y.narrow || p->dtype == VIT_DTYPE_FP32) ? 1 : 2) * UNITS;
   y.width = (p->head_dim <= 64 ? 2 : p->head_dim <= 96 ? 3 : 4) * 32;
   y.part_rows = (int)std::min<int64_t>(rows, most);
-  y.grid = tiles + y.target;
-  // divided requests have more than one share each, so at most twice as many parts as shares
-  y.parts = y.target ? 2 * y.target + p->kv_heads : 0;
-  if (y.target) {
-    auto up = [](size_t n) __attribute__((always_inline)) { return (n + 255) / 256 * 256; };
-    y.head_bytes = up((size_t)p->n_requests * 2 * sizeof(int32_t));
+  // with rows for several rounds of the device there is nothing to divide
+  y.divide = y.narrow || ((int64_t)p->n_rows * group / rows * p->kv_heads < 4 * y.slots && p->table_width > 0);
+  y.grid = y.narrow ? y.slots : tiles + (y.divide ? y.slots : 0);
+  // NARROW: two a workgroup.  WIDE: divided requests have more than one share each, so at most twice as many parts as shares.
+  y.parts = !y.divide ? 0 : 2 * y.slots + (y.narrow ? 0 : p->kv_heads);
+  if (y.divide) {
+    auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+    y.head_bytes = up(((size_t)p->n_requests + 1) * sizeof(int64_t));
     y.stats_bytes = up((size_t)y.parts * y.part_rows * 2 * sizeof(float));
     y.bytes = y.head_bytes + y.stats_bytes + (size_t)y.parts * y.part_rows * y.width * sizeof(float);
   }
@@ -737,8 +1041,12 @@ hipError_t launch_as(const PagedArgs& a, int64_t grid, hipStream_t s) {
   static LdsLimitOnce lds_limit;
   if (hipError_t e = lds_limit.ensure((const void*)kernel, smem); e != hipSuccess) return e;
   hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(THREADS), smem, s, a);
-  if (a.target)
-    hipLaunchKernelGGL((paged_join_kernel<T, DB>), dim3((unsigned)(((int64_t)a.rows * a.heads + 3) / 4)), dim3(256), 0, s, a, Sh::ITEM_ROWS);
+  if (a.divide) {
+    // few rows may have many parts each
+    const int64_t rows = (int64_t)a.rows * a.heads;
+    if (rows <= 16 * UNITS) hipLaunchKernelGGL((paged_join_kernel<T, DB, NARROW, 8>), dim3((unsigned)rows), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_join_kernel<T, DB, NARROW, 1>), dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, s, a);
+  }
   return hipGetLastError();
 }
 
@@ -801,7 +1109,7 @@ extern "C" vit_status_t vit_pages_attend(const vit_pages_attend_t* p, void* stre
   a.q_stride = p->q_stride; a.out_stride = p->out_stride; a.table_stride = p->table_stride;
   a.rows = p->n_rows; a.R = p->n_requests; a.max_new = p->max_new; a.width = p->n_pages > 0 ? p->table_width : 0; a.n_pages = p->n_pages;
   a.shift = __builtin_ctz(p->page_size); a.heads = p->q_heads; a.kv_heads = p->kv_heads; a.group = p->q_heads / p->kv_heads;
-  a.dh = p->head_dim; a.causal = p->causal != 0; a.target = y.target; a.least = 1; a.part_rows = y.part_rows; a.max_parts = y.parts;
+  a.dh = p->head_dim; a.causal = p->causal != 0; a.divide = y.divide; a.slots = __builtin_ctz(y.slots);  a.part_rows = y.part_rows; a.max_parts = y.parts;
   // (a scale of zero: all logits equal, and what no row sees still minus infinity)
   a.scale = std::max(std::fabs(p->scale) * 1.44269504088896340736f, 1e-35f); a.negative = p->scale < 0;
   const hipError_t e = p->dtype == VIT_DTYPE_FP32 ? launch<float>(a, y, (hipStream_t)stream) : launch<bf16_t>(a, y, (hipStream_t)stream);
