@@ -315,7 +315,8 @@ vit_status_t vit_preprocess_tiles(const uint8_t* image, int32_t height, int32_t 
  *                                   Its tokens fill its last page first.  The pages it takes are entered into its row of
  *                                   the block table; nothing else of the table is written.
  *   counts [2]                      entries of free_pages that are taken now (counts may be `taken` itself, for a step
- *                                   that a graph repeats), and the number of new tokens that got no slot.
+ *                                   that a graph repeats), and the number of new tokens that got no slot (2^31 - 1 at
+ *                                   the most).
  * A token whose page would lie past table_width, past the end of free_pages or outside 0 ... n_pages - 1 gets slot -1 (the
  * entry, if there is one for it, becomes -1).  `taken` may be NULL: 0.
  * Outputs overlap neither inputs nor each other, but for the two named.

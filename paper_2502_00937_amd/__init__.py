@@ -24,4 +24,14 @@ from .binding import (  # noqa: F401
     vit_product_time,
     vit_weight_count,
 )
-from .pages import PagePlan, append_pages, attend_pages, plan_pages  # noqa: F401
+
+_PAGES = ("PagePlan", "append_pages", "attend_pages", "plan_pages")
+
+
+def __getattr__(name):  # the paged cache's calls are made of torch tensors: torch is imported with the first of them
+    if name not in _PAGES:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    from . import pages
+
+    globals().update((n, getattr(pages, n)) for n in _PAGES)
+    return globals()[name]

@@ -100,14 +100,10 @@ __device__ __forceinline__ Request request(const PagedArgs& a, int r) {
   return q;
 }
 
-__device__ __forceinline__ int64_t wave_scan(int64_t v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t up = __shfl_up(v, d, 64);
-    if (lane >= d) v += up;
-  }
-  return v;
+// a / b, of numbers that are small as a rule (a division in 64 bits is some hundred instructions)
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  if (((a | b) >> 32) == 0) return (uint32_t)a / (uint32_t)b;
+  return a / b;
 }
 
 // WIDE: workgroup `at` of a head of keys, in the order of the requests, into `found` in LDS; false if there are not so many.
@@ -137,7 +133,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int at, Item& foun
     const Request q = base == 0 ? head : request<ROWS, KEYS>(a, base + tid);
     const int splits = q.steps > share ? 1 + (q.steps - 1) / share : 1;
     const int64_t n = (int64_t)q.tiles * splits, mine = n + (splits > 1 ? n << 32 : 0);
-    const int64_t incl = wave_scan(mine);
+    const int64_t incl = (int64_t)wave_scan((uint64_t)mine);
     if (lane == 63) sums[wave] = incl;
     __syncthreads();
     int64_t before = below + incl - mine;
@@ -183,17 +179,19 @@ __device__ __forceinline__ int workgroup_of(int64_t total, int64_t step, int slo
   return b;
 }
 
-// The request among `from` and the ones behind it that holds step `at`, of which `below` lie before request `from`: its number,
+// Where requests are many: the one among `from` and the ones behind it that holds step `at`, of which `below` lie before request `from`: its number,
 // lengths and the steps before it, into LDS.  With `heads`, the steps before every request are written there.
 struct Stretch { int64_t below; Request q; int r; };
 template <int ROWS, int KEYS>
 __device__ __forceinline__ void find_request(const PagedArgs& a, int from, int64_t below, int64_t at, int64_t* sums, Stretch& out, int64_t* heads) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));  // (nothing of this is kept through the loops over keys)
+  const int lane = tid & 63, wave = tid >> 6;
   if (tid == 0) out.r = -1;
   __syncthreads();
   for (int base = from; base < a.R; base += THREADS) {
     const Request q = request<ROWS, KEYS>(a, base + tid);
-    const int64_t n = (int64_t)q.tiles * q.steps, incl = wave_scan(n);
+    const int64_t n = (int64_t)q.tiles * q.steps, incl = (int64_t)wave_scan((uint64_t)n);
     if (lane == 63) sums[wave] = incl;
     __syncthreads();
     int64_t before = below + incl - n;
@@ -263,7 +261,8 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
   }
 
   Piece qf[KS];
-  const int pieces = a.dh * Sh::ES / 16;  // of a head's row
+  int pieces = a.dh * Sh::ES / 16;  // of a head's row
+  asm volatile("" : "+s"(pieces));  // (what follows from it is worked out where it is used: kept from item to item it is more scalars than there are)
   {
     const int token = row / a.group, head = kv_head * a.group + (row - token * a.group);
     const T* q = (const T*)a.q + (int64_t)(it.start + token) * a.q_stride + (int64_t)head * a.dh;
@@ -327,9 +326,10 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
         const unsigned char* const from = keys0 + (uint64_t)number * page_bytes + (uint32_t)((key + 8 * eight) & ((1 << a.shift) - 1)) * (uint32_t)row_bytes;
         const uint32_t to = base + tile + i * 1024;
         int piece = in_row, at = in_instr;
-        if (!FULL) asm("" : "+v"(piece), "+v"(at));  // compared again every time: kept, the lanes' masks are more scalars than there are
+        if (!FULL) asm volatile("" : "+v"(piece), "+v"(at));  // compared again every time: kept, the lanes' masks are more scalars than there are
         const int row = (NARROW ? 0 : wave * Sh::LOAD) + i * Sh::RPI + at;
         if (FULL || (piece ^ (VALUES ? swv(row) : swk(row))) < pieces) dma16(VALUES ? from + to_values : from, VALUES ? v_from[i] : k_from[i], to);
+        if (i % (8 / Sh::RPI) == 8 / Sh::RPI - 1) __builtin_amdgcn_sched_barrier(0);  // (all addresses at once are more scalars than there are)
       }
     };
     if (full) group(std::true_type{});
@@ -476,7 +476,7 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
   auto weight = [&](float x) __attribute__((always_inline)) { return __builtin_amdgcn_exp2f(fmaf(x, a.scale, neg_m)); };
   auto sum_ones = [&](const uint32_t (&pw)[8]) __attribute__((always_inline)) {
     uint32_t w = two_ones;
-    asm("" : "+v"(w));  // one register between two blocks, not four
+    asm volatile("" : "+v"(w));  // one register between two blocks, not four
     const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{w, w, w, w});
 #pragma unroll
     for (int s2 = 0; s2 < 2; ++s2)
@@ -487,7 +487,7 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
     constexpr bool MASK = decltype(mask_tag)::value;
     // the general block works its places in LDS out again: kept for it, they would be registers that the others have not got
     const uint32_t keep[3] = {k_off, v_off, v_swap};
-    if (MASK) asm("" : "+v"(k_off), "+v"(v_off), "+v"(v_swap));
+    if (MASK) asm volatile("" : "+v"(k_off), "+v"(v_off), "+v"(v_swap));
     f32x16 st = logits(sK);
     if (MASK) {
 #pragma unroll
@@ -553,7 +553,7 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
   };
   auto finish = [&]() __attribute__((always_inline)) {  // the whole sum of a row, in both lanes that share it
     int upper = lane & 16;
-    asm("" : "+v"(upper));
+    asm volatile("" : "+v"(upper));
     if (BF16 && fast) l = upper ? lsum[1] : lsum[0];
     else l += __shfl_xor(l, 32, 64);
   };
@@ -762,7 +762,7 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
   };
   if constexpr (!NARROW) {
     int own_row = row0 + lq;
-    asm("" : "+v"(own_row));  // (worked out here, not ahead of the loops)
+    asm volatile("" : "+v"(own_row));  // (worked out here, not ahead of the loops)
     if (!active || own_row >= in.rows) return;
     const int token = own_row / a.group, head = kv_head * a.group + (own_row - token * a.group);
     const int64_t at = (int64_t)(in.start + token) * a.out_stride + (int64_t)head * a.dh;
@@ -842,41 +842,71 @@ __global__ __launch_bounds__(THREADS, (NARROW || sizeof(T) == 4) && DB > 2 ? 1 :
     if (!find_item<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, blockIdx.x / a.kv_heads, found)) return;
     work_on<T, DB, NARROW>(a, found, blockIdx.x % a.kv_heads, lds);
   } else {
-    __shared__ int64_t sums[4];
+    __shared__ int64_t sums[4], ahead[THREADS + 1];  // steps before each of the first requests, of a head of keys
     __shared__ Stretch stretch;
-    const int tid = threadIdx.x;
-    int64_t steps = 0;  // of a head of keys
-    for (int r = tid; r < a.R; r += THREADS) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const Request mine = request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, tid);
+    int64_t more = 0;
+    for (int r = tid + THREADS; r < a.R; r += THREADS) {
       const Request q = request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, r);
-      steps += (int64_t)q.tiles * q.steps;
+      more += (int64_t)q.tiles * q.steps;
     }
+    const int64_t own = (int64_t)mine.tiles * mine.steps, incl = (int64_t)wave_scan((uint64_t)own);
+    if (lane == 63) sums[wave] = incl;
+    __syncthreads();
+    int64_t before = incl - own;
 #pragma unroll
-    for (int d = 32; d; d >>= 1) steps += __shfl_xor(steps, d, 64);
-    if ((tid & 63) == 0) sums[tid >> 6] = steps;
-    __syncthreads();
-    steps = uniform(sums[0] + sums[1] + sums[2] + sums[3]);
-    __syncthreads();
-    const int64_t total = steps * a.kv_heads, from = first_step(total, blockIdx.x, a.slots), to = first_step(total, blockIdx.x + 1, a.slots);
-    int64_t* const heads = blockIdx.x == 0 ? (int64_t*)a.head : nullptr;
-    if (heads) {
-      if (tid == 0) heads[0] = steps;
-      find_request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, 0, 0, -1, sums, stretch, heads + 1);
+    for (int w = 0; w < 3; ++w)
+      if (w < wave) before += sums[w];
+    ahead[tid] = before;
+    if (tid == THREADS - 1) ahead[THREADS] = before + own;
+    int64_t steps = sums[0] + sums[1] + sums[2] + sums[3];  // of a head of keys
+    if (a.R > THREADS) {
+      more = (int64_t)wave_scan((uint64_t)more);
+      __syncthreads();
+      if (lane == 63) sums[wave] = more;
+      __syncthreads();
+      steps += sums[0] + sums[1] + sums[2] + sums[3];
     }
-    int kv_head = 0, r = 0;
+    steps = uniform(steps);
+    __syncthreads();
+    if (blockIdx.x == 0) {  // for the kernel that joins the parts
+      int64_t* const heads = (int64_t*)a.head;
+      if (tid == 0) heads[0] = steps;
+      if (tid < a.R) heads[1 + tid] = before;
+      if (a.R > THREADS) find_request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, THREADS, ahead[THREADS], -1, sums, stretch, heads + 1);
+    }
+    const int64_t total = steps * a.kv_heads, from = first_step(total, blockIdx.x, a.slots), to = first_step(total, blockIdx.x + 1, a.slots);
+    int kv_head = 0, r = -1;
     int64_t below = 0, at = from;
     if (from < to) {
-      kv_head = (int)(from / steps);
+      kv_head = (int)quotient(from, steps);
       at = from - kv_head * steps;
+      if (before <= at && at < before + own) stretch = Stretch{before, mine, tid};
     }
+    __syncthreads();
 #pragma unroll 1
     for (int64_t done = from; done < to;) {
-      find_request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, r, below, at, sums, stretch, nullptr);
+      if (r < 0 && at < ahead[THREADS]) {
+        // (found above)
+      } else if (at < ahead[THREADS]) {
+        int mine = tid;
+        asm volatile("" : "+v"(mine));  // (its addresses are worked out again)
+        if (ahead[mine] <= at && at < ahead[mine + 1]) stretch = Stretch{ahead[mine], request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, mine), mine};
+        __syncthreads();
+      } else {
+        if (r < THREADS) {
+          r = THREADS;
+          below = ahead[THREADS];
+        }
+        find_request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, r, below, at, sums, stretch, nullptr);
+      }
       r = __builtin_amdgcn_readfirstlane(stretch.r);
       if (r < 0) return;  // (only if the lengths have changed meanwhile)
       below = uniform(stretch.below);
       const Request q = stretch.q;
       const int tiles = __builtin_amdgcn_readfirstlane(q.tiles), its = __builtin_amdgcn_readfirstlane(q.steps);
-      int tile = (int)((at - below) / its), first = (int)(at - below - (int64_t)tile * its);
+      int tile = (int)quotient(at - below, its), first = (int)(at - below - (int64_t)tile * its);
 #pragma unroll 1
       for (; tile < tiles && done < to; ++tile, first = 0) {
         const int last = (int)min((int64_t)its, first + (to - done));

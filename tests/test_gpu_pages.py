@@ -33,7 +33,7 @@ def plain_plan(cached, new, table, free, taken, n_pages, page, rows):
         kv.append(c + fits)
         firsts.append(taken)
     slots += [-1] * (rows - len(slots))
-    return slots, starts, kv, firsts, [min(taken, len(free)), lost], table
+    return slots, starts, kv, firsts, [min(taken, len(free)), min(lost, 2 ** 31 - 1)], table
 
 
 def some_lengths(seed, n, top_cached, top_new):
@@ -55,6 +55,8 @@ PLANS = {
     "wide pages": (*some_lengths(4, 11, 9000, 6000), 4096, 5, 0, 0),
     "rows for fewer": ([3, 60, 8, 1], [20, 50, 9, 4], 8, 20, -25, 0),
     "rows for none": ([3], [20], 8, 20, -20, 0),
+    "rows for several workgroups": ([0, 7, 100], [5000, 3, 9001], 16, 640, 0, 2),
+    "lengths whose sums pass 32 bits": ([2 ** 30, 5, 2 ** 30], [6, 2 ** 30, 2 ** 30], 64, 7, -2 ** 31 + 90, 0),
 }
 
 
@@ -68,6 +70,8 @@ def test_plan(name, trouble):
     say(f"case plan: {name}, {trouble or 'no trouble'}")
     cached, new, page, width, extra, taken = PLANS[name]
     rng = np.random.default_rng(len(name))
+    if name.startswith("lengths") and trouble != "table":
+        width = 2  # (a table of that many pages would be all there is to test)
     rows = sum(max(n, 0) for n in new) + extra + (7 if extra == 0 else 0)
     if trouble == "table":
         width = max(1, width // 2)
