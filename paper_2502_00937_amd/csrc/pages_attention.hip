@@ -42,7 +42,7 @@ struct PagedArgs {
   int64_t max_parts;
   int64_t q_stride, out_stride, table_stride;
   int rows, R, max_new, width, n_pages, shift, heads, kv_heads, group, dh, causal;
-  int divide;    // whether keys are divided
+  int divide;
   int slots;     // logarithm of the workgroups that the device holds at a time, which they are divided for
   int part_rows; // rows of a part
   float scale;   // >= 0, times log2(e)
@@ -111,6 +111,9 @@ template <int ROWS, int KEYS>
 __device__ __forceinline__ bool find_item(const PagedArgs& a, int at, Item& found) {
   __shared__ int64_t sums[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // A part of few steps is mostly its own start and its sums' way through memory: 16 at the least (512 tokens 29.5 us, 30.6 without the
+  // limit; 16 requests of 100 tokens 25.6 and 29; with 32 the 256 tokens over 8000 keys take 67 us for 58).
+  constexpr int LEAST_STEPS = 16;
   int share = INT32_MAX;
   const Request head = request<ROWS, KEYS>(a, tid);
   if (a.divide) {
@@ -125,7 +128,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int at, Item& foun
     __syncthreads();
     work = (sums[0] + sums[1] + sums[2] + sums[3]) * a.kv_heads;
     __syncthreads();
-    share = (int)min(max((work + (1 << a.slots) - 1) >> a.slots, (int64_t)1), (int64_t)INT32_MAX);
+    share = (int)min(max((work + (1 << a.slots) - 1) >> a.slots, (int64_t)LEAST_STEPS), (int64_t)INT32_MAX);
   }
   if (tid == 0) found.r = -1;
   int64_t below = 0;  // places of the requests before, parts of those among them whose keys are divided in the upper half
@@ -1049,8 +1052,10 @@ Layout lay_out(const vit_pages_attend_t* p) {
   y.slots = (p->head_dim > 64 && (y.narrow || p->dtype == VIT_DTYPE_FP32) ? 1 : 2) * UNITS;
   y.width = (p->head_dim <= 64 ? 2 : p->head_dim <= 96 ? 3 : 4) * 32;
   y.part_rows = (int)std::min<int64_t>(rows, most);
-  // with rows for several rounds of the device there is nothing to divide
-  y.divide = y.narrow || ((int64_t)p->n_rows * group / rows * p->kv_heads < 4 * y.slots && p->table_width > 0);
+  // Row tiles that fill the device once leave nothing to divide: a part costs as much as several steps (2048 tokens, 512 tiles of 1 to
+  // 32 steps: 60 us, divided 64; 4096 tokens 165 and 172), below that dividing is what fills it (256 tokens over 8000 keys 58 us,
+  // undivided 152).
+  y.divide = y.narrow || ((int64_t)p->n_rows * group / rows * p->kv_heads < y.slots && p->table_width > 0);
   y.grid = y.narrow ? y.slots : tiles + (y.divide ? y.slots : 0);
   // NARROW: two a workgroup.  WIDE: divided requests have more than one share each, so at most twice as many parts as shares.
   y.parts = !y.divide ? 0 : 2 * y.slots + (y.narrow ? 0 : p->kv_heads);
@@ -1139,7 +1144,7 @@ extern "C" vit_status_t vit_pages_attend(const vit_pages_attend_t* p, void* stre
   a.q_stride = p->q_stride; a.out_stride = p->out_stride; a.table_stride = p->table_stride;
   a.rows = p->n_rows; a.R = p->n_requests; a.max_new = p->max_new; a.width = p->n_pages > 0 ? p->table_width : 0; a.n_pages = p->n_pages;
   a.shift = __builtin_ctz(p->page_size); a.heads = p->q_heads; a.kv_heads = p->kv_heads; a.group = p->q_heads / p->kv_heads;
-  a.dh = p->head_dim; a.causal = p->causal != 0; a.divide = y.divide; a.slots = __builtin_ctz(y.slots);  a.part_rows = y.part_rows; a.max_parts = y.parts;
+  a.dh = p->head_dim; a.causal = p->causal != 0; a.divide = y.divide;  a.slots = __builtin_ctz(y.slots);  a.part_rows = y.part_rows; a.max_parts = y.parts;
   // (a scale of zero: all logits equal, and what no row sees still minus infinity)
   a.scale = std::max(std::fabs(p->scale) * 1.44269504088896340736f, 1e-35f); a.negative = p->scale < 0;
   const hipError_t e = p->dtype == VIT_DTYPE_FP32 ? launch<float>(a, y, (hipStream_t)stream) : launch<bf16_t>(a, y, (hipStream_t)stream);
