@@ -52,6 +52,9 @@ struct PagedArgs {
 typedef const __attribute__((address_space(4))) int32_t* ScalarTable;  // read by scalar loads
 
 constexpr int THREADS = 256;
+// WIDE: a part of few steps is mostly its own start and its sums' way through memory, so it has 16 steps at the least (512 tokens 29.5
+// us, 30.6 without the limit; 16 requests of 100 tokens 25.6 and 29; with 32 steps 256 tokens over 8000 keys take 67 us for 58).
+constexpr int LEAST_STEPS = 16;
 
 template <typename T, int DB_, bool NARROW>
 struct Shape {
@@ -112,25 +115,31 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
 template <int ROWS, int KEYS>
 __device__ __forceinline__ bool find_item(const PagedArgs& a, int at, Item& found) {
   __shared__ int64_t sums[4];
+  __shared__ int most[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  // A part of few steps is mostly its own start and its sums' way through memory: 16 at the least (512 tokens 29.5 us, 30.6 without the
-  // limit; 16 requests of 100 tokens 25.6 and 29; with 32 the 256 tokens over 8000 keys take 67 us for 58).
-  constexpr int LEAST_STEPS = 16;
   int share = INT32_MAX;
   const Request head = request<ROWS, KEYS>(a, tid);
   if (a.divide) {
     int64_t work = (int64_t)head.tiles * head.steps;
+    int longest = head.tiles ? head.steps : 0;
     for (int r = tid + THREADS; r < a.R; r += THREADS) {
       const Request q = request<ROWS, KEYS>(a, r);
       work += (int64_t)q.tiles * q.steps;
+      if (q.tiles) longest = max(longest, q.steps);
     }
+    work = (int64_t)wave_scan((uint64_t)work);
 #pragma unroll
-    for (int d = 32; d; d >>= 1) work += __shfl_xor(work, d, 64);
-    if (lane == 0) sums[wave] = work;
+    for (int d = 32; d; d >>= 1) longest = max(longest, __shfl_xor(longest, d, 64));
+    if (lane == 63) {
+      sums[wave] = work;
+      most[wave] = longest;
+    }
     __syncthreads();
     work = (sums[0] + sums[1] + sums[2] + sums[3]) * a.kv_heads;
+    longest = max(max(most[0], most[1]), max(most[2], most[3]));
     __syncthreads();
     share = (int)min(max((work + (1 << a.slots) - 1) >> a.slots, (int64_t)LEAST_STEPS), (int64_t)INT32_MAX);
+    if (blockIdx.x == 0 && tid == 0) a.head[0] = longest > share;  // whether there is anything to join
   }
   if (tid == 0) found.r = -1;
   int64_t below = 0;  // places of the requests before, parts of those among them whose keys are divided in the upper half
@@ -240,8 +249,8 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 31, g = lane >> 5;
   if (!NARROW && a.head && tid == 0 && kv_head == 0 && it.tile == 0 && it.split == 0) {
-    a.head[2 * it.r] = it.part;
-    a.head[2 * it.r + 1] = it.splits;
+    a.head[2 + 2 * it.r] = it.part;
+    a.head[3 + 2 * it.r] = it.splits;
   }
 
   // ---- rows: this lane's, and how many keys it sees
@@ -943,12 +952,10 @@ __global__ __launch_bounds__(THREADS, (NARROW || sizeof(T) == 4) && DB > 2 ? 1 :
 // loads' latencies are what this kernel is.  HALVES of them share a row: one where rows are many, all eight of a
 // workgroup where they are few and may have many parts each.
 template <typename T, int DB, bool NARROW, int HALVES>
-__global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
+__device__ __forceinline__ void join_row(const PagedArgs& a, uint32_t i) {
   using Sh = Shape<T, DB, NARROW>;
   const int half = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t i = HALVES == 1 ? (int64_t)blockIdx.x * 8 + half : blockIdx.x;
-  const int t = (int)(i / a.heads), head = (int)(i - (int64_t)t * a.heads);
-  if (t >= a.rows) return;
+  const int t = (int)(i / (uint32_t)a.heads), head = (int)(i - (uint32_t)t * a.heads);
   int lo = 0, hi = a.R;  // of the requests lo .. hi - 1 one is the last to start at t or below
   while (hi - lo > 1) {
     const int step = (hi - lo + 31) / 32, at = lo + lane * step;
@@ -977,8 +984,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
     second = 2 * (b0 + 1) - part;
     next = 2;
   } else {
-    const int first = a.head[2 * lo];
-    splits = a.head[2 * lo + 1];
+    const int first = a.head[2 + 2 * lo];
+    splits = a.head[3 + 2 * lo];
     if (first < 0) return;
     part = ((int64_t)first + (int64_t)tile * splits) * a.kv_heads + kv_head;  // the others lie kv_heads parts apart
     second = next = a.kv_heads;
@@ -1034,6 +1041,16 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
   else *(f32x4*)((float*)a.out + at) = f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv};
 }
 
+template <typename T, int DB, bool NARROW, int HALVES>
+__global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
+  if (!NARROW && a.head[0] == 0) return;  // no request's keys were divided
+  const uint32_t rows = (uint32_t)a.rows * a.heads, at_once = HALVES == 1 ? 8 : 1;  // (rows: below 2^31)
+  for (uint32_t i = blockIdx.x * at_once + (HALVES == 1 ? threadIdx.x >> 5 : 0); i < rows; i += gridDim.x * at_once) {
+    join_row<T, DB, NARROW, HALVES>(a, i);
+    if constexpr (HALVES > 1) __syncthreads();  // before LDS is used again
+  }
+}
+
 // ---- host ---------------------------------------------------------------------------------
 // How a call is laid out: by the sizes that the host knows, upper bounds of what the device finds.
 struct Layout {
@@ -1056,10 +1073,7 @@ Layout lay_out(const vit_pages_attend_t* p) {
   y.slots = (p->head_dim > 64 && (y.narrow || p->dtype == VIT_DTYPE_FP32) ? 1 : 2) * UNITS;
   y.width = (p->head_dim <= 64 ? 2 : p->head_dim <= 96 ? 3 : 4) * 32;
   y.part_rows = (int)std::min<int64_t>(rows, most);
-  // Row tiles that fill the device once leave nothing to divide: a part costs as much as several steps (2048 tokens, 512 tiles of 1 to
-  // 32 steps: 60 us, divided 64; 4096 tokens 165 and 172), below that dividing is what fills it (256 tokens over 8000 keys 58 us,
-  // undivided 152).
-  y.divide = y.narrow || ((int64_t)p->n_rows * group / rows * p->kv_heads < y.slots && p->table_width > 0);
+  y.divide = y.narrow || (int64_t)p->table_width * p->page_size > LEAST_STEPS * 64;  // (there may be something to divide)
   y.grid = y.narrow ? y.slots : tiles + (y.divide ? y.slots : 0);
   // NARROW: two a workgroup.  WIDE: divided requests have more than one share each, so at most twice as many parts as shares.
   y.parts = !y.divide ? 0 : 2 * y.slots + (y.narrow ? 0 : p->kv_heads);
@@ -1084,7 +1098,7 @@ hipError_t launch_as(const PagedArgs& a, int64_t grid, hipStream_t s) {
     // few rows may have many parts each
     const int64_t rows = (int64_t)a.rows * a.heads;
     if (rows <= 16 * UNITS) hipLaunchKernelGGL((paged_join_kernel<T, DB, NARROW, 8>), dim3((unsigned)rows), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((paged_join_kernel<T, DB, NARROW, 1>), dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_join_kernel<T, DB, NARROW, 1>), dim3((unsigned)std::min<int64_t>((rows + 7) / 8, 8 * UNITS)), dim3(256), 0, s, a);
   }
   return hipGetLastError();
 }
