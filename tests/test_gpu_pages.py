@@ -91,8 +91,9 @@ def test_plan(name, trouble):
     assert t[:, :width].tolist() == want[5].tolist() and (t[:, width:] == -77).all()
 
 
-def test_plan_of_a_step_that_is_repeated_in_place():
-    """kv_lens over cached_lens and counts over taken, eagerly and from a graph: every replay is the next step."""
+@pytest.mark.parametrize("padding", [3, 5000])
+def test_plan_of_a_step_that_is_repeated_in_place(padding):
+    """kv_lens over cached_lens and counts over taken, eagerly and from a graph: every replay is the next step.  (Few rows and many.)"""
     import torch
 
     import paper_2502_00937_amd as V
@@ -108,7 +109,7 @@ def test_plan_of_a_step_that_is_repeated_in_place():
         table[r, :held] = order[at:at + held]
         at += held
     new = rng.integers(0, 4, n)
-    rows = int(new.sum()) + 3
+    rows = int(new.sum()) + padding
     free = order[at:]
     lens, counts, t, d_new, d_free = dev(cached), dev([0, 0]), dev(table), dev(new), dev(free)
     plan = V.PagePlan(dev([0] * rows), dev([0] * (n + 1)), lens, dev([0] * (n + 1)), counts)
@@ -375,9 +376,56 @@ def test_attend_writes_its_rows_alone(dtype):
     assert V.attend_pages(**dict(c, q=c["q"][:0])).shape == (0, 6, 72)
 
 
-def test_attend_many_requests():
-    lens = [(1, 1 + (37 * i) % 211) for i in range(1500)] + [(3, 40)]
-    check(make_case("bf16", 4, 2, 64, 16, lens), lens, True, what="1501 requests")
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("last", [3, 200])
+def test_attend_many_requests(dtype, last):
+    """More requests than a workgroup has threads, in either form."""
+    lens = [(1, 1 + (37 * i) % 211) for i in range(700)] + [(0, 9), (last, last + 37)] + [(1, 1 + (91 * i) % 1300) for i in range(90)]
+    check(make_case(dtype, 12, 4, 64, 16, lens), lens, True, what=f"{len(lens)} requests")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,kv_heads,dim", [(8, 2, 128), (14, 2, 64), (24, 4, 88)])
+def test_attend_chunks_beside_long_single_tokens(dtype, causal, heads, kv_heads, dim):
+    lens = [(1, 6000), (200, 3000), (1, 64), (40, 1500), (1, 20000), (3, 5), (600, 600)]
+    check(make_case(dtype, heads, kv_heads, dim, 16, lens), lens, causal, what=f"chunks and tokens {heads} / {kv_heads} x {dim}")
+
+
+def test_attend_requests_that_share_pages():
+    """A common beginning lies in the pool once; what each request has behind it does not."""
+    import torch
+
+    import paper_2502_00937_amd as V
+
+    lens = [(1, 400), (9, 400), (70, 400), (1, 400)]
+    for part in (lens[:2], lens):
+        c = make_case("bf16", 8, 2, 64, 16, part, garbage=False)
+        shared = c["block_table"].clone()
+        shared[1:, :17] = shared[0, :17]
+        got = V.attend_pages(**dict(c, block_table=shared))
+        for r in range(1, len(part)):  # the same keys in pages of each request's own
+            for pool in (c["key_pages"], c["value_pages"]):
+                pool[c["block_table"][r, :17].long()] = pool[shared[0, :17].long()]
+        assert torch.equal(got, V.attend_pages(**c))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("fresh", [2, 60])
+def test_attend_lengths_that_the_table_has_no_room_for(dtype, fresh):
+    """Keys past the table's last page are not there; a negative number of keys is none."""
+    import torch
+
+    import paper_2502_00937_amd as V
+
+    lens = [(fresh, 64), (fresh, 64), (fresh, 0)]
+    c = make_case(dtype, 8, 2, 64, 16, lens)
+    c["block_table"] = c["block_table"][:, :4].contiguous()
+    want = V.attend_pages(**c, causal=False)
+    for causal in (True, False):
+        got = V.attend_pages(**dict(c, kv_lens=dev([1000, 2 ** 31 - 1, -5])), causal=causal)
+        assert torch.equal(got, want), causal
+    assert (want[2 * fresh:] == 0).all()
 
 
 def test_offsets_past_32_bits():
