@@ -505,7 +505,8 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
     const uint32_t keep[3] = {k_off, v_off, v_swap};
     if (MASK) asm volatile("" : "+v"(k_off), "+v"(v_off), "+v"(v_swap));
     f32x16 st = logits(sK);
-    if (MASK) {
+    const bool hidden = MASK && (key0 + 32 > all_see || bad);  // some row does not see some key
+    if (hidden) {
 #pragma unroll
       for (int v = 0; v < 16; ++v)
         if (key0 + 8 * (v >> 2) + 4 * g + (v & 3) >= seen || (bad >> (v >> 2) & 1)) st[v] = -INFINITY;
@@ -543,7 +544,7 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
       }
     }
     if (BF16 && (!MASK || fast)) sum_ones(pw);
-    if (MASK && any_no_number(sV)) accumulate_around(sV, pw, pf, st);
+    if (hidden && any_no_number(sV)) accumulate_around(sV, pw, pf, st);
     else accumulate(sV, pw, pf);
     k_off = keep[0];
     v_off = keep[1];
