@@ -323,17 +323,20 @@ vit_status_t vit_preprocess_tiles(const uint8_t* image, int32_t height, int32_t 
  *
  * vit_pages_append: rows i of k and v (head h's values at i * stride + h * head_dim) to slots[i] of the pools.  Rows with a slot
  * outside 0 ... n_pages * page_size - 1 are passed over.  No slot may be given twice.  Pointers and rows are multiples of
- * 16 bytes.
+ * 16 bytes.  The rows' values of k are below 64 GiB together.
  *
  * vit_pages_attend: rows query_offsets[r] ... query_offsets[r + 1] - 1 of q and out are request r's; row i's head h (at
  * i * stride + h * head_dim) attends to its request's kv_lens[r] keys of head h / (q_heads / kv_heads):
  *   out = sum_j softmax_j(scale * q . k_j) v_j,
  * over all keys, or with `causal` over those up to its own, where the request's rows are the last of its keys.  A row
- * that sees no key gets zeros.  What no row may see (keys past kv_lens or past a row's own, other pages, pages whose number
- * lies outside 0 ... n_pages - 1) has no effect, infinities and NaN among it.  Rows behind the last request's are left as they
+ * that sees no key gets zeros.  What no row may see (keys past kv_lens, past table_width pages or past a row's own, other pages,
+ * pages whose number lies outside 0 ... n_pages - 1) has no effect, infinities and NaN among it.  Lengths are 0 to 2^31 - 256 (a
+ * negative one counts as 0, a larger one as that).  Rows behind the last request's are left as they
  * are.  max_new: no request has more rows (of one that has, those past max_new are left as they are).  Logits, softmax and
- * sums are fp32; in bf16 the weights are rounded to bf16 ahead of the second product.  The keys' axis is divided
- * by what the batch leaves of the device, so the last bits of a row depend on the batch, never on timing.
+ * sums are fp32 (of more than 2^24 keys of like weight that one part holds, the last lose their share of it); in bf16 the weights are rounded to bf16 ahead of the second product.  The keys' axis is divided
+ * by what the batch leaves of the device and its parts are joined in order, so the last bits of a row depend on the batch, never on
+ * timing.  The lengths and the table must not change while the call is at work.
+ * n_rows * q_heads is below 2^31, n_requests * kv_heads plus the row tiles (of 128 rows of a request and head of keys) below 2^24 - 512.
  * head_dim is a multiple of 8, at most 128; q_heads a multiple of kv_heads; scale finite; pointers and rows multiples of 16 bytes.
  * vit_pages_attend_query: bytes of workspace that the call needs (pointers in the struct are not looked at); the workspace is
  * 256-byte aligned, its contents undefined before and after, and no two calls at work at a time may share it.

@@ -292,7 +292,8 @@ extern "C" vit_status_t vit_pages_append(const vit_pages_append_t* p, void* stre
   a.rows = p->n_rows; a.n_slots = p->n_pages * p->page_size; a.shift = __builtin_ctz(p->page_size);
   a.heads = p->kv_heads; a.per_head = p->head_dim * es / 16;
   const int64_t groups = ((int64_t)a.rows * a.heads * a.per_head + 255) / 256;
-  if (groups > INT32_MAX) return set_error(VIT_EINVAL, "vit_pages_append: too many rows");
+  if (groups >= 1 << 24)  // (a launch has fewer than 2^32 threads)
+    return set_error(VIT_EINVAL, "vit_pages_append: rows of k must be below 64 GiB together");
   hipLaunchKernelGGL(append_kernel, dim3((unsigned)groups, 2), dim3(256), 0, (hipStream_t)stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return set_error(VIT_EDEVICE, "vit_pages_append: launch: %s", hipGetErrorString(e));

@@ -52,6 +52,7 @@ struct PagedArgs {
 typedef const __attribute__((address_space(4))) int32_t* ScalarTable;  // read by scalar loads
 
 constexpr int THREADS = 256;
+constexpr int MOST_KEYS = INT32_MAX - 255;  // of a request: a few steps behind its last key, numbers of keys still fit 31 bits
 // WIDE: a part of few steps is mostly its own start and its sums' way through memory, so it has 16 steps at the least (512 tokens 29.5
 // us, 30.6 without the limit; 16 requests of 100 tokens 25.6 and 29; with 32 steps 256 tokens over 8000 keys take 67 us for 58).
 constexpr int LEAST_STEPS = 16;
@@ -95,7 +96,7 @@ __device__ __forceinline__ Request request(const PagedArgs& a, int r) {
     q.start = a.starts[r];
     const int64_t n = (int64_t)a.starts[r + 1] - q.start;
     q.fresh = q.start < 0 || n < 0 || q.start + n > a.rows ? 0 : (int)n;
-    q.kv = max(a.kv[r], 0);
+    q.kv = min(max(a.kv[r], 0), MOST_KEYS);
     q.tiles = (int)(((int64_t)min(q.fresh, a.max_new) * a.group + ROWS - 1) / ROWS);
     // (at least one: rows that see nothing have to be written)
     q.steps = max((int)((min((int64_t)q.kv, (int64_t)a.width << a.shift) + KEYS - 1) / KEYS), 1);
@@ -919,11 +920,12 @@ __global__ __launch_bounds__(THREADS, (NARROW || sizeof(T) == 4) && DB > 2 ? 1 :
         find_request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, r, below, at, sums, stretch, nullptr);
       }
       r = __builtin_amdgcn_readfirstlane(stretch.r);
-      if (r < 0) return;  // (only if the lengths have changed meanwhile)
       below = uniform(stretch.below);
       const Request q = stretch.q;
       const int tiles = __builtin_amdgcn_readfirstlane(q.tiles), its = __builtin_amdgcn_readfirstlane(q.steps);
+      if (r < 0 || its < 1) return;  // (only if the lengths have changed meanwhile: nothing is right then, but it ends)
       int tile = (int)quotient(at - below, its), first = (int)(at - below - (int64_t)tile * its);
+      if (tile >= tiles) return;  // (likewise)
 #pragma unroll 1
       for (; tile < tiles && done < to; ++tile, first = 0) {
         const int last = (int)min((int64_t)its, first + (to - done));
@@ -1120,6 +1122,7 @@ vit_status_t check_sizes(const vit_pages_attend_t* p, const char* name) {
     return set_error(VIT_EINVAL, "%s: q_heads must be a multiple of kv_heads, at most 1024", name);
   if (p->n_rows < 0 || p->n_rows >= 1 << 30 || p->n_requests < 0 || p->n_requests > 1 << 20 || p->max_new < 0 || p->table_width < 0)
     return set_error(VIT_EINVAL, "%s: sizes must not be negative, n_rows < 2^30, n_requests <= 2^20", name);
+  if (!std::isfinite(p->scale)) return set_error(VIT_EINVAL, "%s: scale must be finite", name);
   // so that numbers of rows, row tiles and workgroups stay inside 31 bits
   if ((int64_t)p->n_rows * p->q_heads >= (int64_t)1 << 31 || (int64_t)p->n_requests * p->kv_heads >= 1 << 30)
     return set_error(VIT_EINVAL, "%s: n_rows * q_heads must be below 2^31, n_requests * kv_heads below 2^30", name);
@@ -1140,9 +1143,8 @@ extern "C" vit_status_t vit_pages_attend(const vit_pages_attend_t* p, void* stre
   if (vit_status_t st = check_sizes(p, "vit_pages_attend"); st != VIT_OK) return st;
   const int es = p->dtype == VIT_DTYPE_FP32 ? 4 : 2, row = p->q_heads * p->head_dim;
   if (p->q_stride < row || p->out_stride < row || p->q_stride > (int64_t)1 << 32 || p->out_stride > (int64_t)1 << 32 ||
-      p->table_stride < p->table_width || !std::isfinite(p->scale))
-    return set_error(VIT_EINVAL, "vit_pages_attend: strides of q and out must be q_heads * head_dim to 2^32, table_stride >= table_width, "
-                                 "scale finite");
+      p->table_stride < p->table_width)
+    return set_error(VIT_EINVAL, "vit_pages_attend: strides of q and out must be q_heads * head_dim to 2^32, table_stride >= table_width");
   if (p->n_rows == 0 || p->n_requests == 0 || p->max_new == 0) return VIT_OK;
   if (!p->q || !p->out || !p->query_offsets || !p->kv_lens || (p->table_width > 0 && !p->block_table) ||
       (p->n_pages > 0 && (!p->key_pages || !p->value_pages)))
@@ -1151,6 +1153,8 @@ extern "C" vit_status_t vit_pages_attend(const vit_pages_attend_t* p, void* stre
       (p->out_stride * es & 15) || ((uintptr_t)p->workspace & 255))
     return set_error(VIT_EINVAL, "vit_pages_attend: pointers and rows must be multiples of 16 bytes, the workspace 256-byte aligned");
   const Layout y = lay_out(p);
+  if (y.grid >= 1 << 24)  // (a launch has fewer than 2^32 threads)
+    return set_error(VIT_EINVAL, "vit_pages_attend: more requests and rows than a launch has workgroups for");
   if (y.bytes && (!p->workspace || p->workspace_bytes < y.bytes))
     return set_error(VIT_ECAPACITY, "vit_pages_attend: workspace holds %zu bytes, %zu needed", p->workspace ? p->workspace_bytes : 0, y.bytes);
   PagedArgs a;

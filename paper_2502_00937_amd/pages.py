@@ -77,6 +77,13 @@ def _rows(name, t, dtype, device, dim, heads=None):
     return n, h, row if n > 1 else max(row, h * d)
 
 
+def _pack(layout: struct.Struct, *fields) -> bytes:
+    try:
+        return layout.pack(*fields)
+    except (struct.error, OverflowError) as e:  # a number that its field does not hold, or none at all
+        _refuse(f"argument out of range: {e}")
+
+
 def _call(function, packed: bytes, device: int) -> None:
     if device < 0:
         _refuse("the tensors must be on a GPU")
@@ -113,7 +120,7 @@ def plan_pages(cached_lens, new_lens, block_table, free_pages, taken, n_pages: i
                 _refuse(f"the plan's {name} holds {t.numel()} numbers, {size} needed")
         places = tuple(t.data_ptr() for t in out)
     _call(load_library().vit_pages_plan,
-          _PLAN.pack(cached_lens.data_ptr(), new_lens.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(),
+          _pack(_PLAN, cached_lens.data_ptr(), new_lens.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(),
                      0 if taken is None else taken.data_ptr(), *places, stride, n, width, n_free, n_pages, page_size, n_rows), device)
     return out
 
@@ -127,13 +134,14 @@ def append_pages(k, v, slots, key_pages, value_pages) -> None:
     if not n == n_v == _vector("slots", slots, device):
         _refuse(f"k, v and slots have {n}, {n_v} and {slots.numel()} rows")
     _call(load_library().vit_pages_append,
-          _APPEND.pack(k.data_ptr(), v.data_ptr(), slots.data_ptr(), key_pages.data_ptr(), value_pages.data_ptr(), k_row, v_row, n,
+          _pack(_APPEND, k.data_ptr(), v.data_ptr(), slots.data_ptr(), key_pages.data_ptr(), value_pages.data_ptr(), k_row, v_row, n,
                        n_pages, page_size, heads, dim, dtype), device)
 
 
 def attend_pages(q, key_pages, value_pages, block_table, query_offsets, kv_lens, max_new: int, causal: bool = True, scale=None, out=None):
     """Attention of the rows of `q` ([rows, q_heads, head_dim]) over their requests' keys and values in the pools: see
-    `vit_pages_attend`.  `scale` is 1 / sqrt(head_dim) if not given.  Returns `out`, [rows, q_heads, head_dim]."""
+    `vit_pages_attend`.  `scale` is 1 / sqrt(head_dim) if not given.  Returns `out`, [rows, q_heads, head_dim]; no gradient
+    passes through it."""
     dtype, device, n_pages, kv_heads, page_size, dim = _pools(key_pages, value_pages)
     n, heads, q_row = _rows("q", q, key_pages.dtype, device, dim)
     requests, width, stride = _table(block_table, device)
@@ -150,9 +158,9 @@ def attend_pages(q, key_pages, value_pages, block_table, query_offsets, kv_lens,
                 kv_lens.data_ptr(), out.data_ptr())
     sizes = (q_row, out_row, stride, n, requests, max_new, width, n_pages, page_size, heads, kv_heads, dim, 1 if causal else 0, dtype,
              dim ** -0.5 if scale is None else scale)
-    _check(lib.vit_pages_attend_query(_ATTEND.pack(*pointers, 0, 0, *sizes), C.byref(need)))
+    _check(lib.vit_pages_attend_query(_pack(_ATTEND, *pointers, 0, 0, *sizes), C.byref(need)))
     bytes_needed = need.value
     # from torch's allocator, call by call: another stream's or graph's calls have workspaces of their own
     workspace = query_offsets.new_empty(bytes_needed // 4) if bytes_needed else None
-    _call(lib.vit_pages_attend, _ATTEND.pack(*pointers, workspace.data_ptr() if bytes_needed else 0, bytes_needed, *sizes), device)
+    _call(lib.vit_pages_attend, _pack(_ATTEND, *pointers, workspace.data_ptr() if bytes_needed else 0, bytes_needed, *sizes), device)
     return out

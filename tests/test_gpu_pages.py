@@ -428,6 +428,33 @@ def test_attend_lengths_that_the_table_has_no_room_for(dtype, fresh):
     assert (want[2 * fresh:] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("fresh", [1, 600])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attend_as_many_keys_as_a_length_holds(dtype, fresh, causal):
+    """2^31 - 1 keys (taken as 2^31 - 256) of a table that names one page again and again.  Its keys are zeros and its values ones:
+    the weights are ones, their sums and those of the values the same whole numbers in the same order, of which 1 / sum
+    and the product with it are each rounded once, (1 + 2^-24)^2 - 1 < 2^-22; in bf16 that is 1.
+
+    600 rows in fp32 are 5 row tiles of 2^25 steps on 512 workgroups: parts of 5 * 2^25 / 512 * 64 = 20971520 keys.  Values are added up
+    one by one, and an fp32 sum of ones stops at 2^24, where one more is half of its step; weights are two lanes' sums of
+    half as many and do not.  So a part's quotient is 2^24 / 20971520 = 1 - 0.2 at the least.  (In bf16 sixteen are added at a
+    time, which is a whole number of steps up to 2^28.)"""
+    import torch
+
+    import paper_2502_00937_amd as V
+
+    say(f"case as many keys as a length holds: {dtype}, {fresh} rows, {'causal' if causal else 'all'}")
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    pools = [torch.full((2, 1, 4096, 8), x, dtype=t, device="cuda") for x in (0.0, 1.0)]
+    pools[1][0] = float("nan")  # (a page that the table does not name)
+    q = torch.randn(fresh, 1, 8, device="cuda").to(t)
+    table = torch.ones(1, 1 << 19, dtype=torch.int32, device="cuda")
+    got = V.attend_pages(q, *pools, table, dev([0, fresh]), dev([2 ** 31 - 1]), fresh, causal=causal)
+    stops = 1 - 2 ** 24 / 20971520 if dtype == "fp32" and fresh == 600 else 0
+    assert (got.double() - 1).abs().max().item() <= (0 if dtype == "bf16" else 2 ** -22 + stops)
+
+
 def test_offsets_past_32_bits():
     """Pools of more than 2^32 bytes and 2^31 values: pages at both ends."""
     import torch

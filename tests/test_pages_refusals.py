@@ -114,6 +114,25 @@ def test_binding_refuses_tensors_that_do_not_fit():
     assert "counts" in refused(V.plan_pages, ints(2), ints(2), ints(2, 4), ints(3), None, 6, 16, 7, out=wrong)
 
 
+def test_launches_that_have_no_room_are_refused():
+    """More threads than a launch has (2^32): an error ahead of the launch, not one of it."""
+    lib = V.load_library()
+    assert append(lib, rows=1 << 23, heads=32, dim=128, k_stride=4096, v_stride=4096) == -1
+    assert b"64 GiB" in lib.vit_last_error()
+    assert attend(lib, rows=1 << 26, n=1 << 20, max_new=1 << 10, heads=16, kv_heads=16, q_stride=1024, out_stride=1024) == -1
+    assert b"workgroups" in lib.vit_last_error()
+
+
+@pytest.mark.parametrize("number", [2 ** 31, -2 ** 31 - 1, 2 ** 70, 1.5])
+def test_binding_refuses_numbers_that_no_field_holds(number):
+    pool = torch.zeros(6, 2, 16, 64, dtype=torch.bfloat16)
+    q = torch.zeros(5, 4, 64, dtype=torch.bfloat16)
+    assert "range" in refused(V.attend_pages, q, pool, pool, ints(2, 4), ints(3), ints(2), number)
+    assert "range" in refused(V.plan_pages, ints(2), ints(2), ints(2, 4), ints(3), None, number, 16, 7)
+    assert "range" in refused(V.plan_pages, ints(2), ints(2), ints(2, 4), ints(3), None, 6, number, 7)
+    assert "scale" in refused(V.attend_pages, q, pool, pool, ints(2, 4), ints(3), ints(2), 3, scale=1e39)  # (infinite as a float)
+
+
 def test_structs_match_the_header():
     """The packed formats follow include/vitenc.h: field sizes in order."""
     import os
