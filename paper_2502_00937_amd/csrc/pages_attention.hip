@@ -9,14 +9,17 @@
 // in blocks of 32 keys x 32 rows: in bf16 on 32 x 32 x 16 matrix instructions, V^T by the transposing LDS read, in fp32 on
 // 32 x 32 x 2 ones.
 //
-// Two forms.  WIDE: 128 rows a workgroup, 32 a wave, which share tiles of keys.  NARROW, where no request has more than 32
-// rows (single tokens): the waves share the rows and each has keys of its own, so that four times as many loads are on
-// their way and no barrier stands between them; their results are joined in LDS.
+// Two forms.  WIDE: 128 rows a workgroup, 32 a wave, which share tiles of 64 keys; bound by the matrix units at the device's power limit
+// (4096 rows of 128 columns over 32768 keys 1.12 PFLOP/s; the causal half of 8192 tokens 0.98).  NARROW, where requests have few
+// rows: the waves share 32 rows and each has keys of its own, so that four times as many loads are on their way and no
+// barrier stands between them; bound by HBM (64 single tokens over 2.09 GB of keys and values 5.76 TB/s).
 //
-// Work is divided on the device, where the lengths are: every workgroup adds up the key tiles of all requests, which gives
-// the share of a request's keys that one workgroup takes (all of them, where there are rows enough), and finds its own
-// place in that order.  A request whose keys are divided leaves parts (sums without division, their reference maximum and
-// sum of weights) in the workspace, which a second kernel joins, always in the same order.
+// Work is divided on the device, where the lengths are: every workgroup adds up the steps of all requests and finds its own
+// place.  NARROW: the steps of all requests, one after the other, are dealt out evenly, one run of them a workgroup (a part of a
+// request's keys each before: 8 tokens over 50000 keys 315 us, now 284).  WIDE: a workgroup is one row tile, whose
+// keys are divided if they are longer than an even share of all work (runs as in NARROW are two starts and two parts a
+// workgroup: 2048 tokens 97 us for 60).  What is divided leaves parts (sums without division, their reference maximum and sum of
+// weights) in the workspace, which a second kernel joins, always in the same order.
 //
 // Keys and values go from their pages to LDS without passing registers (global_load_lds_dwordx4: 1 KiB of LDS a wave and
 // instruction, each lane naming its 16 bytes).  Eight consecutive keys lie in one page, so that pages are looked up by
@@ -35,8 +38,9 @@ struct PagedArgs {
   const void *q, *kp, *vp;
   void* out;
   const int32_t *table, *starts, *kv;
-  // workspace, all nullptr if no request's keys are divided: (first part, parts) of every request, reference maximum and
-  // sum of every part's rows, their unnormalised values
+  // workspace, all nullptr if no request's keys can be divided.  What the join needs to know (NARROW, int64: the steps of a head
+  // of keys, then the steps before each request; WIDE, int32: whether anything was divided, nothing, then every request's
+  // first part and parts); reference maximum and sum of every part's rows; their unnormalised values
   int32_t* head;
   float *stats, *parts;
   int64_t max_parts;
@@ -69,7 +73,8 @@ struct Shape {
   static constexpr int INSTR = LOAD / RPI;                   // load instructions for K, and for V
   static constexpr int PAGES = LOAD / 8;                     // pages it looks up
   static constexpr int TILE = KEYS * ROWB;                   // bytes of LDS of a tile of K or V
-  // NARROW: tiles on their way at a time, of K and of V, for each wave.  (WIDE: two of either.)
+  // NARROW: tiles on their way at a time, of K and of V, for each wave: two in bf16; in fp32, twice the bytes, one, so that two workgroups
+  // lie on a unit up to 64 columns (text over images 109 us, with two 133).  (WIDE: two of either.)
   static constexpr int NS = NARROW && ES == 4 ? 1 : 2;
   static constexpr int LDS = (NARROW ? 4 : 1) * NS * 2 * TILE;
   static constexpr int ITEM_ROWS = NARROW ? 32 : 128;
@@ -951,7 +956,7 @@ __global__ __launch_bounds__(THREADS, (NARROW || sizeof(T) == 4) && DB > 2 ? 1 :
   }
 }
 
-// The parts of a row whose request's keys were divided, in order.  Half a wave takes a part, 16 bytes a lane, four parts at a time: the
+// The parts of a row whose request's keys were divided, in order (one token over 131072 keys, 512 parts: 6.2 us).  Half a wave takes a part, 16 bytes a lane, four parts at a time: the
 // loads' latencies are what this kernel is.  HALVES of them share a row: one where rows are many, all eight of a
 // workgroup where they are few and may have many parts each.
 template <typename T, int DB, bool NARROW, int HALVES>
@@ -1070,9 +1075,13 @@ Layout lay_out(const vit_pages_attend_t* p) {
   Layout y{};
   const int group = p->q_heads / p->kv_heads;
   const int64_t most = (int64_t)p->max_new * group;  // rows of a request and head of keys
+  // NARROW reads keys once for every 32 rows, WIDE for every 128 but with barriers and with idle waves below.  bf16: above 32 rows WIDE
+  // (8 requests of 64 rows 62 us, NARROW 101).  fp32's products take nine times as long, which hides the reads for longer:
+  // requests of up to 360 rows over 577 keys each in NARROW 107 us, in WIDE 183; with 128 columns 425 and 534.
   y.narrow = most <= (p->dtype == VIT_DTYPE_FP32 ? 512 : 32);
   const int rows = y.narrow ? 32 : 128;
   const int64_t tiles = p->kv_heads * std::min<int64_t>((most + rows - 1) / rows * p->n_requests, (int64_t)p->n_rows * group / rows + p->n_requests);
+  // workgroups that LDS and registers let the device hold
   y.slots = (p->head_dim > 64 && (y.narrow || p->dtype == VIT_DTYPE_FP32) ? 1 : 2) * UNITS;
   y.width = (p->head_dim <= 64 ? 2 : p->head_dim <= 96 ? 3 : 4) * 32;
   y.part_rows = (int)std::min<int64_t>(rows, most);
