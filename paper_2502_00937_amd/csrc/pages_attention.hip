@@ -77,8 +77,10 @@ struct Shape {
   // lie on a unit up to 64 columns (text over images 109 us, with two 133).  (WIDE: two of either.)
   static constexpr int NS = NARROW && ES == 4 ? 1 : 2;
   static constexpr int LDS = (NARROW ? 4 : 1) * NS * 2 * TILE;
-  static constexpr int ITEM_ROWS = NARROW ? 32 : 128;
-  static constexpr int ITEM_KEYS = NARROW ? 128 : 64;        // keys of a step of the whole workgroup
+  // NARROW in fp32: up to 64 rows, by two pairs of waves that have the same keys, half as many a step
+  static constexpr int PAIRS = NARROW && ES == 4 ? 2 : 1;
+  static constexpr int ITEM_ROWS = NARROW ? 32 * PAIRS : 128;
+  static constexpr int ITEM_KEYS = NARROW ? 128 : 64;        // keys of a step of the whole workgroup, if its waves all have their own
 };
 
 // ---- a workgroup's place ------------------------------------------------------------------
@@ -91,20 +93,26 @@ struct Item {
 };
 
 struct Request {
-  int start, fresh, kv, tiles, steps;
+  int start, fresh, kv, tiles;
+  int steps, last;  // of a row tile's keys; of the last tile's
+  __device__ __forceinline__ int64_t all() const { return tiles ? (int64_t)(tiles - 1) * steps + last : 0; }
+  __device__ __forceinline__ int of(int tile) const { return tile == tiles - 1 ? last : steps; }
 };
 
-template <int ROWS, int KEYS>
+template <typename Sh>
 __device__ __forceinline__ Request request(const PagedArgs& a, int r) {
-  Request q{0, 0, 0, 0, 0};
+  constexpr int ROWS = Sh::ITEM_ROWS, KEYS = Sh::ITEM_KEYS;
+  Request q{0, 0, 0, 0, 0, 0};
   if (r < a.R) {
     q.start = a.starts[r];
     const int64_t n = (int64_t)a.starts[r + 1] - q.start;
     q.fresh = q.start < 0 || n < 0 || q.start + n > a.rows ? 0 : (int)n;
     q.kv = min(max(a.kv[r], 0), MOST_KEYS);
-    q.tiles = (int)(((int64_t)min(q.fresh, a.max_new) * a.group + ROWS - 1) / ROWS);
+    const int64_t rows = (int64_t)min(q.fresh, a.max_new) * a.group, keys = min((int64_t)q.kv, (int64_t)a.width << a.shift);
+    q.tiles = (int)((rows + ROWS - 1) / ROWS);
     // (at least one: rows that see nothing have to be written)
-    q.steps = max((int)((min((int64_t)q.kv, (int64_t)a.width << a.shift) + KEYS - 1) / KEYS), 1);
+    q.steps = q.last = max((int)((keys + KEYS / Sh::PAIRS - 1) / (KEYS / Sh::PAIRS)), 1);
+    if (Sh::PAIRS > 1 && rows - (int64_t)(q.tiles - 1) * ROWS <= 32) q.last = max((int)((keys + KEYS - 1) / KEYS), 1);
   }
   return q;
 }
@@ -118,18 +126,18 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
 // WIDE: workgroup `at` of a head of keys into `found` in LDS; false if there are not so many.  The requests whose rows are one wave's
 // come first: beside the others they cost little, behind them they are the launch's end (a chunk of 2048 tokens as the first request
 // and 24 single tokens behind it 349 us, in the requests' own order 385).
-template <int ROWS, int KEYS>
+template <typename Sh>
 __device__ __forceinline__ bool find_item(const PagedArgs& a, int at, Item& found) {
   __shared__ int64_t sums[4];
   __shared__ int most[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int share = INT32_MAX;
-  const Request head = request<ROWS, KEYS>(a, tid);
+  const Request head = request<Sh>(a, tid);
   if (a.divide) {
     int64_t work = (int64_t)head.tiles * head.steps;
     int longest = head.tiles ? head.steps : 0;
     for (int r = tid + THREADS; r < a.R; r += THREADS) {
-      const Request q = request<ROWS, KEYS>(a, r);
+      const Request q = request<Sh>(a, r);
       work += (int64_t)q.tiles * q.steps;
       if (q.tiles) longest = max(longest, q.steps);
     }
@@ -151,7 +159,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int at, Item& foun
   int64_t below = 0;  // places of the requests before, parts of those among them whose keys are divided in the upper half
   for (int few = 1; few >= 0; --few) {
     for (int base = 0; base < a.R; base += THREADS) {
-      const Request q = base == 0 ? head : request<ROWS, KEYS>(a, base + tid);
+      const Request q = base == 0 ? head : request<Sh>(a, base + tid);
       const int rows = min(q.fresh, a.max_new) * a.group, splits = q.steps > share ? 1 + (q.steps - 1) / share : 1;
       const int64_t n = (rows <= 32) == (few != 0) ? (int64_t)q.tiles * splits : 0, mine = n + (splits > 1 ? n << 32 : 0);
       const int64_t incl = (int64_t)wave_scan((uint64_t)mine);
@@ -204,7 +212,7 @@ __device__ __forceinline__ int workgroup_of(int64_t total, int64_t step, int slo
 // Where requests are many: the one among `from` and the ones behind it that holds step `at`, of which `below` lie before request `from`: its number,
 // lengths and the steps before it, into LDS.  With `heads`, the steps before every request are written there.
 struct Stretch { int64_t below; Request q; int r; };
-template <int ROWS, int KEYS>
+template <typename Sh>
 __device__ __forceinline__ void find_request(const PagedArgs& a, int from, int64_t below, int64_t at, int64_t* sums, Stretch& out, int64_t* heads) {
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));  // (nothing of this is kept through the loops over keys)
@@ -212,8 +220,8 @@ __device__ __forceinline__ void find_request(const PagedArgs& a, int from, int64
   if (tid == 0) out.r = -1;
   __syncthreads();
   for (int base = from; base < a.R; base += THREADS) {
-    const Request q = request<ROWS, KEYS>(a, base + tid);
-    const int64_t n = (int64_t)q.tiles * q.steps, incl = (int64_t)wave_scan((uint64_t)n);
+    const Request q = request<Sh>(a, base + tid);
+    const int64_t n = q.all(), incl = (int64_t)wave_scan((uint64_t)n);
     if (lane == 63) sums[wave] = incl;
     __syncthreads();
     int64_t before = below + incl - n;
@@ -265,7 +273,9 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
     if (!a.causal) return all;
     return max(min(all, it.kv - it.fresh + row / a.group + 1), 0);
   };
-  const int row0 = it.tile * Sh::ITEM_ROWS + (NARROW ? 0 : wave * 32);
+  const bool pairs = Sh::PAIRS > 1 && it.rows - it.tile * Sh::ITEM_ROWS > 32;  // NARROW: two pairs of waves have rows and keys in common
+  const int item_keys = pairs ? Sh::ITEM_KEYS / Sh::PAIRS : Sh::ITEM_KEYS, keys_of = pairs ? wave & 1 : wave;
+  const int row0 = it.tile * Sh::ITEM_ROWS + (!NARROW ? wave * 32 : pairs ? (wave >> 1) * 32 : 0);
   const int row = min(row0 + lq, it.rows - 1);
   const bool active = __builtin_amdgcn_readfirstlane(row0 < it.rows);
   const int seen = sees(row);
@@ -311,7 +321,7 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
   const ScalarTable table = (ScalarTable)(uintptr_t)(a.table + (int64_t)it.r * a.table_stride);
   const int last_entry = max(tile_sees - 1, 0) >> a.shift;
   struct Pages { int number[Sh::PAGES]; };
-  auto step_key = [&](int step) __attribute__((always_inline)) { return step * Sh::ITEM_KEYS + wave * Sh::LOAD; };  // the first key that the wave loads
+  auto step_key = [&](int step) __attribute__((always_inline)) { return step * item_keys + keys_of * Sh::LOAD; };  // the first key that the wave loads
   auto look_up = [&](int step) __attribute__((always_inline)) {
     Pages p;
     const int key = step_key(step);
@@ -743,7 +753,7 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
 
   // a row that sees keys of this part and whose sum is out of range
   auto out_of_range = [&]() __attribute__((always_inline)) {
-    const bool sees_some = first * Sh::ITEM_KEYS < seen;
+    const bool sees_some = first * item_keys < seen;
     return __builtin_amdgcn_ballot_w64(sees_some && !(l >= 0x1p-100f && l <= 0x1p100f)) != 0;
   };
   if constexpr (NARROW) {
@@ -810,7 +820,7 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
     float* const ms = (float*)lds;              // [4][32] maxima, [4][32] sums
     float* const so = (float*)(lds + 1024);     // [4][32][32 DB + 4]: rows a bank apart
     constexpr int LD = DB * 32 + 4;
-    const int rows = min(32, in.rows - row0);
+    const int rows = min(32, in.rows - row0), tile_row = in.tile * Sh::ITEM_ROWS, tile_rows = min(Sh::ITEM_ROWS, in.rows - tile_row);
     if (g == 0) {
       ms[wave * 32 + lq] = m;
       ms[128 + wave * 32 + lq] = l;
@@ -824,24 +834,26 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
     }
     __syncthreads();
     constexpr int QUADS = DB * 8;
-    for (int i = tid; i < rows * QUADS; i += THREADS) {
+    for (int i = tid; i < tile_rows * QUADS; i += THREADS) {
       const int r = i / QUADS, col = (i - r * QUADS) * 4;
-      float top = ms[r];
+      const int at = pairs ? r + (r & 32) : r, waves = pairs ? 2 : 4;  // the first wave that has the row, its numbers' place; how many have
+      float top = ms[at];
 #pragma unroll
-      for (int w = 1; w < 4; ++w) top = fmaxf(top, ms[w * 32 + r]);
+      for (int w = 1; w < 4; ++w)
+        if (w < waves) top = fmaxf(top, ms[w * 32 + at]);
       const float ref = top == -INFINITY ? 0.f : top;
       f32x4 v = {0.f, 0.f, 0.f, 0.f};
       float sum = 0.f;
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        if (ms[128 + w * 32 + r] == 0.f) continue;  // it saw nothing
-        const float mw = ms[w * 32 + r], f = __builtin_amdgcn_exp2f((mw == -INFINITY ? 0.f : mw) - ref);
-        const f32x4 x = *(const f32x4*)(so + (w * 32 + r) * LD + col);
+        if (w >= waves || ms[128 + w * 32 + at] == 0.f) continue;  // (it saw nothing)
+        const float mw = ms[w * 32 + at], f = __builtin_amdgcn_exp2f((mw == -INFINITY ? 0.f : mw) - ref);
+        const f32x4 x = *(const f32x4*)(so + (w * 32 + at) * LD + col);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = fmaf(x[e], f, v[e]);
-        sum = fmaf(ms[128 + w * 32 + r], f, sum);
+        sum = fmaf(ms[128 + w * 32 + at], f, sum);
       }
-      const int tok = (row0 + r) / a.group, hd = kv_head * a.group + (row0 + r - tok * a.group);
+      const int tok = (tile_row + r) / a.group, hd = kv_head * a.group + (tile_row + r - tok * a.group);
       if (part >= 0) {
         *(f32x4*)(a.parts + (part * a.part_rows + r) * (DB * 32) + col) = v;
         if (col == 0) {
@@ -862,19 +874,19 @@ __global__ __launch_bounds__(THREADS, (NARROW || sizeof(T) == 4) && DB > 2 ? 1 :
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   __shared__ Item found;
   if constexpr (!NARROW) {
-    if (!find_item<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, blockIdx.x / a.kv_heads, found)) return;
+    if (!find_item<Sh>(a, blockIdx.x / a.kv_heads, found)) return;
     work_on<T, DB, NARROW>(a, found, blockIdx.x % a.kv_heads, lds);
   } else {
     __shared__ int64_t sums[4], ahead[THREADS + 1];  // steps before each of the first requests, of a head of keys
     __shared__ Stretch stretch;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const Request mine = request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, tid);
+    const Request mine = request<Sh>(a, tid);
     int64_t more = 0;
     for (int r = tid + THREADS; r < a.R; r += THREADS) {
-      const Request q = request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, r);
-      more += (int64_t)q.tiles * q.steps;
+      const Request q = request<Sh>(a, r);
+      more += q.all();
     }
-    const int64_t own = (int64_t)mine.tiles * mine.steps, incl = (int64_t)wave_scan((uint64_t)own);
+    const int64_t own = mine.all(), incl = (int64_t)wave_scan((uint64_t)own);
     if (lane == 63) sums[wave] = incl;
     __syncthreads();
     int64_t before = incl - own;
@@ -897,7 +909,7 @@ __global__ __launch_bounds__(THREADS, (NARROW || sizeof(T) == 4) && DB > 2 ? 1 :
       int64_t* const heads = (int64_t*)a.head;
       if (tid == 0) heads[0] = steps;
       if (tid < a.R) heads[1 + tid] = before;
-      if (a.R > THREADS) find_request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, THREADS, ahead[THREADS], -1, sums, stretch, heads + 1);
+      if (a.R > THREADS) find_request<Sh>(a, THREADS, ahead[THREADS], -1, sums, stretch, heads + 1);
     }
     const int64_t total = steps * a.kv_heads, from = first_step(total, blockIdx.x, a.slots), to = first_step(total, blockIdx.x + 1, a.slots);
     int kv_head = 0, r = -1;
@@ -915,28 +927,28 @@ __global__ __launch_bounds__(THREADS, (NARROW || sizeof(T) == 4) && DB > 2 ? 1 :
       } else if (at < ahead[THREADS]) {
         int mine = tid;
         asm volatile("" : "+v"(mine));  // (its addresses are worked out again)
-        if (ahead[mine] <= at && at < ahead[mine + 1]) stretch = Stretch{ahead[mine], request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, mine), mine};
+        if (ahead[mine] <= at && at < ahead[mine + 1]) stretch = Stretch{ahead[mine], request<Sh>(a, mine), mine};
         __syncthreads();
       } else {
         if (r < THREADS) {
           r = THREADS;
           below = ahead[THREADS];
         }
-        find_request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, r, below, at, sums, stretch, nullptr);
+        find_request<Sh>(a, r, below, at, sums, stretch, nullptr);
       }
       r = __builtin_amdgcn_readfirstlane(stretch.r);
       below = uniform(stretch.below);
       const Request q = stretch.q;
-      const int tiles = __builtin_amdgcn_readfirstlane(q.tiles), its = __builtin_amdgcn_readfirstlane(q.steps);
+      const int tiles = __builtin_amdgcn_readfirstlane(q.tiles), its = __builtin_amdgcn_readfirstlane(q.steps), last_its = __builtin_amdgcn_readfirstlane(q.last);
       if (r < 0 || its < 1) return;  // (only if the lengths have changed meanwhile: nothing is right then, but it ends)
-      int tile = (int)quotient(at - below, its), first = (int)(at - below - (int64_t)tile * its);
-      if (tile >= tiles) return;  // (likewise)
+      int tile = min((int)quotient(at - below, its), tiles - 1), first = (int)(at - below - (int64_t)tile * its);
+      if (tile < 0 || first >= (tile == tiles - 1 ? last_its : its)) return;  // (likewise)
 #pragma unroll 1
       for (; tile < tiles && done < to; ++tile, first = 0) {
-        const int last = (int)min((int64_t)its, first + (to - done));
+        const int end = tile == tiles - 1 ? last_its : its, last = (int)min((int64_t)end, first + (to - done));
         if (tid == 0) {
           // a workgroup leaves a part of its first item and one of its last at the most
-          const int part = first == 0 && last == its ? -1 : 2 * (int)blockIdx.x + (done == from ? 0 : 1);
+          const int part = first == 0 && last == end ? -1 : 2 * (int)blockIdx.x + (done == from ? 0 : 1);
           found = Item{r, tile, 0, 1, first, last, part, q.start, q.fresh, q.kv, min(q.fresh, a.max_new) * a.group};
         }
         __syncthreads();
@@ -945,7 +957,7 @@ __global__ __launch_bounds__(THREADS, (NARROW || sizeof(T) == 4) && DB > 2 ? 1 :
         done += last - first;
         at += last - first;
       }
-      below += (int64_t)tiles * its;
+      below += (int64_t)(tiles - 1) * its + last_its;
       ++r;
       if (at == steps) {
         ++kv_head;
@@ -983,8 +995,9 @@ __device__ __forceinline__ void join_row(const PagedArgs& a, uint32_t i) {
   if constexpr (NARROW) {
     const int64_t* const heads = (const int64_t*)a.head;
     const int64_t steps = heads[0];
-    const int its = request<Sh::ITEM_ROWS, Sh::ITEM_KEYS>(a, lo).steps;
-    const int64_t total = steps * a.kv_heads, at = kv_head * steps + heads[1 + lo] + (int64_t)tile * its;
+    const Request q = request<Sh>(a, lo);
+    const int its = q.of(tile);
+    const int64_t total = steps * a.kv_heads, at = kv_head * steps + heads[1 + lo] + (int64_t)tile * q.steps;
     const int b0 = workgroup_of(total, at, a.slots), b1 = workgroup_of(total, at + its - 1, a.slots);
     splits = b1 - b0 + 1;
     if (splits < 2) return;
@@ -1079,7 +1092,7 @@ Layout lay_out(const vit_pages_attend_t* p) {
   // (8 requests of 64 rows 62 us, NARROW 101).  fp32's products take nine times as long, which hides the reads for longer:
   // requests of up to 360 rows over 577 keys each in NARROW 107 us, in WIDE 183; with 128 columns 425 and 534.
   y.narrow = most <= (p->dtype == VIT_DTYPE_FP32 ? 512 : 32);
-  const int rows = y.narrow ? 32 : 128;
+  const int rows = !y.narrow ? 128 : p->dtype == VIT_DTYPE_FP32 ? 64 : 32;
   const int64_t tiles = p->kv_heads * std::min<int64_t>((most + rows - 1) / rows * p->n_requests, (int64_t)p->n_rows * group / rows + p->n_requests);
   // workgroups that LDS and registers let the device hold
   y.slots = (p->head_dim > 64 && (y.narrow || p->dtype == VIT_DTYPE_FP32) ? 1 : 2) * UNITS;
