@@ -515,12 +515,14 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
       lsum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, __builtin_bit_cast(bf16x8, u32x4{pw[4 * s2], pw[4 * s2 + 1], pw[4 * s2 + 2], pw[4 * s2 + 3]}),
                                                      lsum, 0, 0, 0);
   };
-  auto block = [&](auto mask_tag, const unsigned char* sK, const unsigned char* sV, int key0, uint32_t bad) __attribute__((always_inline)) {
+  // `between`: what is done once K's tile has been read and before V's is
+  auto block = [&](auto mask_tag, const unsigned char* sK, const unsigned char* sV, int key0, uint32_t bad, auto&& between) __attribute__((always_inline)) {
     constexpr bool MASK = decltype(mask_tag)::value;
     // the general block works its places in LDS out again: kept for it, they would be registers that the others have not got
     const uint32_t keep[3] = {k_off, v_off, v_swap};
     if (MASK) asm volatile("" : "+v"(k_off), "+v"(v_off), "+v"(v_swap));
     f32x16 st = logits(sK);
+    between();
     const bool hidden = MASK && (key0 + 32 > all_see || bad);  // some row does not see some key
     if (hidden) {
 #pragma unroll
@@ -569,10 +571,12 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
   const std::true_type YES{};
   const std::false_type NO{};
   // a block at key0, of which the wave's rows see all, some or none
-  auto any_block = [&](const unsigned char* sK, const unsigned char* sV, int key0, uint32_t bad) __attribute__((always_inline)) {
-    if (fast && begun && key0 + 32 <= all_see && !bad) block(NO, sK, sV, key0, 0);
-    else if (key0 < some_see) block(YES, sK, sV, key0, bad);
+  auto any_block = [&](const unsigned char* sK, const unsigned char* sV, int key0, uint32_t bad, auto&& between) __attribute__((always_inline)) {
+    if (fast && begun && key0 + 32 <= all_see && !bad) block(NO, sK, sV, key0, 0, between);
+    else if (key0 < some_see) block(YES, sK, sV, key0, bad, between);
+    else between();
   };
+  auto nothing = []() __attribute__((always_inline)) {};
 
   auto clear = [&]() __attribute__((always_inline)) {
     m = -INFINITY;
@@ -683,7 +687,7 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
             for (int i = 0; i < 4; ++i)
               bad |= (unsigned)table[min((key0 + 8 * i) >> a.shift, last_entry)] < (unsigned)a.n_pages ? 0u : 1u << i;
           }
-          if (key0 < some_see) block(YES, lds + k_at(t) + kb * 32 * ROWB, lds + v_at(t) + kb * 32 * ROWB, key0, bad);
+          if (key0 < some_see) block(YES, lds + k_at(t) + kb * 32 * ROWB, lds + v_at(t) + kb * 32 * ROWB, key0, bad, nothing);
         }
       }
       __syncthreads();
@@ -719,32 +723,55 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
     if (work) finish();
     __syncthreads();  // before the buffers are used again
   };
-  // NARROW: a wave waits for its own loads alone, of which a stage more is on its way.
+  // NARROW: a wave waits for its own loads alone, of which a stage more is on its way.  With one tile of K and of V, K's next one is
+  // loaded as soon as K has been read, behind the first product, and V's behind the second: either has a product's time.
   auto narrow_pass = [&]() __attribute__((always_inline)) {
     clear();
-    constexpr int LOADS = 2 * Sh::INSTR;
     uint32_t bad[2] = {0u, 0u};
     auto load_both = [&](int t, const Pages& p, int s) __attribute__((always_inline)) {
       bad[s] = bad_pages(p);
       load(NO, t, p, s * 2 * Sh::TILE);
       load(YES, t, p, (s * 2 + 1) * Sh::TILE);
     };
+    auto read = []() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };  // reads of LDS are through
 #pragma unroll
     for (int s = 0; s < Sh::NS; ++s)
       if (first + s < last) load_both(first + s, look_up(first + s), s);
-    for (int t0 = first; t0 < last; t0 += Sh::NS) {
-#pragma unroll
-      for (int s = 0; s < Sh::NS; ++s) {
-        const int t = t0 + s;
-        if (t >= last) break;
+    if constexpr (Sh::NS == 1) {
+      for (int t = first; t < last; ++t) {
         Pages p{};
-        if (t + Sh::NS < last) p = look_up(t + Sh::NS);
-        if (Sh::NS > 1 && t + 1 < last) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
-        else wait();
-        any_block(mine + s * 2 * Sh::TILE, mine + (s * 2 + 1) * Sh::TILE, step_key(t), bad[s]);
-        if (t + Sh::NS < last) {
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the block's reads of this stage are through
-          load_both(t + Sh::NS, p, s);
+        if (t + 1 < last) p = look_up(t + 1);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Sh::INSTR) : "memory");  // K is there, V perhaps not
+        any_block(mine, mine + Sh::TILE, step_key(t), bad[0], [&]() __attribute__((always_inline)) {
+          if (t + 1 < last) {
+            read();
+            load(NO, t + 1, p, 0);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Sh::INSTR) : "memory");  // V is there, the next K perhaps not
+          } else {
+            wait();
+          }
+        });
+        if (t + 1 < last) {
+          read();
+          bad[0] = bad_pages(p);
+          load(YES, t + 1, p, Sh::TILE);
+        }
+      }
+    } else {
+      for (int t0 = first; t0 < last; t0 += Sh::NS) {
+#pragma unroll
+        for (int s = 0; s < Sh::NS; ++s) {
+          const int t = t0 + s;
+          if (t >= last) break;
+          Pages p{};
+          if (t + Sh::NS < last) p = look_up(t + Sh::NS);
+          if (t + 1 < last) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * Sh::INSTR) : "memory");
+          else wait();
+          any_block(mine + s * 2 * Sh::TILE, mine + (s * 2 + 1) * Sh::TILE, step_key(t), bad[s], nothing);
+          if (t + Sh::NS < last) {
+            read();
+            load_both(t + Sh::NS, p, s);
+          }
         }
       }
     }
