@@ -74,7 +74,7 @@ struct Shape {
   static constexpr int PAGES = LOAD / 8;                     // pages it looks up
   static constexpr int TILE = KEYS * ROWB;                   // bytes of LDS of a tile of K or V
   // NARROW: tiles on their way at a time, of K and of V, for each wave: two in bf16; in fp32, twice the bytes, one, so that two workgroups
-  // lie on a unit up to 64 columns (text over images 109 us, with two 133).  (WIDE: two of either.)
+  // lie on a unit up to 64 columns (with two, text over images took 133 us where it took 109).  (WIDE: two of either.)
   static constexpr int NS = NARROW && ES == 4 ? 1 : 2;
   static constexpr int LDS = (NARROW ? 4 : 1) * NS * 2 * TILE;
   // NARROW in fp32: up to 64 rows, by two pairs of waves that have the same keys, half as many a step
@@ -285,8 +285,10 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
   const int tile_sees = __builtin_amdgcn_readfirstlane(sees(min(it.tile * Sh::ITEM_ROWS + Sh::ITEM_ROWS - 1, it.rows - 1)));
   // this workgroup's steps of ITEM_KEYS keys
   int first = it.first, last = it.last;
-  if (!NARROW) {
-    const int steps = (tile_sees + Sh::ITEM_KEYS - 1) / Sh::ITEM_KEYS;
+  const int steps = (tile_sees + item_keys - 1) / item_keys;
+  if (NARROW) {  // (not those that no row of the tile sees, which are dealt out like the others)
+    last = max(min(last, steps), first);
+  } else {
     const int even = steps / it.splits, more = steps - even * it.splits;  // the first `more` parts have a step more
     first = __builtin_amdgcn_readfirstlane(it.split * even + min(it.split, more));
     last = __builtin_amdgcn_readfirstlane(first + even + (it.split < more ? 1 : 0));
@@ -1115,9 +1117,11 @@ Layout lay_out(const vit_pages_attend_t* p) {
   Layout y{};
   const int group = p->q_heads / p->kv_heads;
   const int64_t most = (int64_t)p->max_new * group;  // rows of a request and head of keys
-  // NARROW reads keys once for every 32 rows, WIDE for every 128 but with barriers and with idle waves below.  bf16: above 32 rows WIDE
-  // (8 requests of 64 rows 62 us, NARROW 101).  fp32's products take nine times as long, which hides the reads for longer:
-  // requests of up to 360 rows over 577 keys each in NARROW 107 us, in WIDE 183; with 128 columns 425 and 534.
+  // NARROW reads keys once for every 32 rows (fp32: 64), WIDE for every 128 but with barriers and with idle waves where rows are fewer.
+  // bf16: above 32 rows WIDE (8 requests of 64 rows 62 us, NARROW 101).  fp32's products take nine times as long, which hides the reads
+  // for longer: 24 requests of 4 to 360 rows, 128 columns, over images in NARROW 354 us, in WIDE 517; 4 of 400 rows over 2000 keys 165
+  // and 183; 1000 rows over 4000 keys 191 and 176.  (Prompts with nothing cached would be better off in WIDE, 8 of 200 tokens 28.6 us for
+  // 41.8, 4 of 500 172 for 206: shares of a causal triangle are not even.  But only the device knows that they are.)
   y.narrow = most <= (p->dtype == VIT_DTYPE_FP32 ? 512 : 32);
   const int rows = !y.narrow ? 128 : p->dtype == VIT_DTYPE_FP32 ? 64 : 32;
   const int64_t tiles = p->kv_heads * std::min<int64_t>((most + rows - 1) / rows * p->n_requests, (int64_t)p->n_rows * group / rows + p->n_requests);
