@@ -392,6 +392,20 @@ def test_attend_chunks_beside_long_single_tokens(dtype, causal, heads, kv_heads,
     check(make_case(dtype, heads, kv_heads, dim, 16, lens), lens, causal, what=f"chunks and tokens {heads} / {kv_heads} x {dim}")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("heads,kv_heads,dim,lens", [
+    (4, 4, 64, [(32, 500), (33, 500), (64, 64), (65, 700), (96, 96), (97, 2500), (1, 2000), (31, 31), (40, 10), (34, 0), (63, 1), (128, 129)]),
+    (3, 3, 72, [(512, 512), (33, 40), (0, 9), (480, 3300), (1, 1)]),
+    (12, 2, 128, [(5, 900), (6, 33), (11, 7000), (16, 16), (17, 1000), (85, 90), (1, 130)]),
+    (7, 1, 40, [(64, 4000)]),
+])
+def test_attend_row_tiles_of_one_and_two_waves(dtype, causal, heads, kv_heads, dim, lens):
+    """Rows around 32 and 64 and their multiples, where the last tile of a request is of one sort or the other, few and many keys."""
+    c = make_case(dtype, heads, kv_heads, dim, 16, lens)
+    check(c, lens, causal, what=f"row tiles {heads} / {kv_heads} x {dim}")
+
+
 def test_attend_requests_that_share_pages():
     """A common beginning lies in the pool once; what each request has behind it does not."""
     import torch
