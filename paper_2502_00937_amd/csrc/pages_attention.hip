@@ -495,7 +495,7 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
     }
   };
 
-  // Weights are exp2(x - m) with the maximum m of the row's first block for all of its keys, which serves any row whose sum of
+  // Weights are exp2(x - m) with the maximum m of the row's first block (of which some row sees a key) for all of its keys, which serves any row whose sum of
   // weights stays between 2^-100 and 2^100 (bf16 and fp32 have the same exponents, so nothing is lost); a wave with another
   // row goes over its keys again with a running maximum (`fast` is false then).
   bool fast = true, begun = false;
@@ -547,7 +547,8 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
           for (int v = 0; v < 16; ++v) o[b][v] *= shrink;
       }
       m = up;
-      begun = true;
+      // (a block that hides its keys from all rows, by its pages' numbers, leaves nothing: the next one is the first)
+      begun = begun || __builtin_amdgcn_ballot_w64(m != -INFINITY) != 0;
       neg_m = m == -INFINITY ? 0.f : -m;
     }
     uint32_t pw[8];
@@ -698,6 +699,7 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
       ++t;
       if ((t & 1) || t + 1 >= hot_end) continue;
       if (work) {
+        begun = true;  // (the references are those there are from here on)
         Piece kf[KS];
         f32x16 s0 = logits(lds), s1;
 #pragma unroll
@@ -781,10 +783,11 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
     finish();
   };
 
-  // a row that sees keys of this part and whose sum is out of range
+  // a row that sees keys of this part and whose sum is out of range, or whose weights were measured against no maximum at all: its logits
+  // in the first block were minus infinity.  (So that wherever sums are joined, one that is not zero has a reference.)
   auto out_of_range = [&]() __attribute__((always_inline)) {
     const bool sees_some = first * item_keys < seen;
-    return __builtin_amdgcn_ballot_w64(sees_some && !(l >= 0x1p-100f && l <= 0x1p100f)) != 0;
+    return __builtin_amdgcn_ballot_w64(sees_some && (m == -INFINITY || !(l >= 0x1p-100f && l <= 0x1p100f))) != 0;
   };
   if constexpr (NARROW) {
     if (all == 0) {

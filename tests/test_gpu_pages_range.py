@@ -1,0 +1,72 @@
+"""The paged cache at the ends of its types' range and of its lengths: against plain implementations in 64 bits."""
+import numpy as np
+import pytest
+
+from parity_util import say
+from test_gpu_pages import compare, dev, make_case, plain_attend, plain_plan
+
+pytestmark = pytest.mark.gpu
+
+
+def set_logits(c, lens, logits):
+    """Queries of ones, keys of equal numbers: with a scale of 1, key j of request r has the logit logits[r][j] for every row (as far as
+    the type holds a dim-th of it).  Pages outside the pool are passed over."""
+    import torch
+
+    page, dim, n_pages = c["key_pages"].shape[2], c["q"].shape[2], c["key_pages"].shape[0]
+    c["q"] = torch.ones_like(c["q"])
+    for r, (_, keys) in enumerate(lens):
+        at = torch.arange(keys, device="cuda")
+        numbers = c["block_table"][r].long()[at // page]
+        held = (numbers >= 0) & (numbers < n_pages)
+        k = (torch.as_tensor(logits[r], dtype=torch.float64, device="cuda") / dim).to(c["q"].dtype)[held]
+        c["key_pages"][numbers[held], :, (at % page)[held]] = k[:, None, None].expand(-1, c["key_pages"].shape[1], dim)
+
+
+def check_range(c, lens, causal, scale, what):
+    import paper_2502_00937_amd as V
+
+    want, tol = plain_attend(c, lens, causal, scale)
+    compare(V.attend_pages(**c, causal=causal, scale=scale), want, tol, what)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("late,others", [(0.0, -150.0), (0.0, -95.0), (40.0, -60.0), (-60.0, -150.0), (-10.0, 10.0)])
+def test_first_keys_of_a_wave_in_pages_outside_the_pool(dtype, late, others):
+    """Keys 0 to 31, the first that one wave works on, are hidden by their pages' numbers; that wave's later keys lie far above (or
+    below) the other waves', whose references must not be measured against a reference that nobody has seen.  64 requests of 8
+    heads and 4 steps: several steps a workgroup, whatever the number of workgroups."""
+    lens = [(1, 512)] * 64
+    c = make_case(dtype, 8, 8, 64, 16, lens)
+    c["block_table"][:, :2] = -1
+    logits = np.full(512, others)
+    logits[np.arange(512) % 128 < 32] = late
+    set_logits(c, lens, [logits] * 64)
+    for causal in (True, False):
+        check_range(c, lens, causal, 1.0, f"wave's first keys hidden, later {late}, others {others}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_first_keys_of_a_part_in_pages_outside_the_pool(dtype):
+    """One token over 1024 steps of 128 keys, two steps a part: in every seventh part the first step is hidden, in the others its logits are
+    -125; the second step's are -62 in all parts, so all of these weigh the same.  Their values tell the parts apart."""
+    lens = [(1, 131072)]
+    c = make_case(dtype, 1, 1, 64, 16, lens)
+    entries = np.arange(131072 // 16)
+    seventh = entries // 16 % 7 == 5
+    table = c["block_table"][0, :len(entries)].long()
+    c["value_pages"][table] = dev(np.where(seventh, 1, -1)).to(c["q"].dtype)[:, None, None, None].expand(-1, 1, 16, 64)
+    c["block_table"][0, np.nonzero(seventh & (entries % 16 < 8))[0]] = 2 ** 31 - 1
+    set_logits(c, lens, [np.where(np.arange(131072) % 256 < 128, -125.0, -62.0)])
+    check_range(c, lens, True, 1.0, "part's first keys hidden")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("fresh", [1, 20, 130, 700])
+def test_pages_that_were_given_up(dtype, fresh):
+    """A request's first pages have left the pool (-1 in its table), as far as into the last step: the others are all there is."""
+    lens = [(fresh, 2000)] * 3
+    c = make_case(dtype, 4, 2, 64, 16, lens)
+    for r, gone in enumerate((16, 39, 79)):
+        c["block_table"][r, :gone] = -1
+    check_range(c, lens, True, 64 ** -0.5, f"{fresh} rows, first pages given up")
