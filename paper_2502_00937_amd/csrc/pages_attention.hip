@@ -495,7 +495,7 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
     }
   };
 
-  // Weights are exp2(x - m) with the maximum m of the row's first block (of which some row sees a key) for all of its keys, which serves any row whose sum of
+  // Weights are exp2(x - m) with the maximum m of the row's first block for all of its keys, which serves any row whose sum of
   // weights stays between 2^-100 and 2^100 (bf16 and fp32 have the same exponents, so nothing is lost); a wave with another
   // row goes over its keys again with a running maximum (`fast` is false then).
   bool fast = true, begun = false;
@@ -547,8 +547,7 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
           for (int v = 0; v < 16; ++v) o[b][v] *= shrink;
       }
       m = up;
-      // (a block that hides its keys from all rows, by its pages' numbers, leaves nothing: the next one is the first)
-      begun = begun || __builtin_amdgcn_ballot_w64(m != -INFINITY) != 0;
+      begun = true;
       neg_m = m == -INFINITY ? 0.f : -m;
     }
     uint32_t pw[8];
@@ -574,10 +573,12 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
   };
   const std::true_type YES{};
   const std::false_type NO{};
-  // a block at key0, of which the wave's rows see all, some or none
+  // A block at key0, of which the wave's rows see all, some or none.  One whose pages all lie outside the pool is passed over, the first
+  // one above all: it would leave its rows without a reference.
+  constexpr uint32_t NOTHING = 15;
   auto any_block = [&](const unsigned char* sK, const unsigned char* sV, int key0, uint32_t bad, auto&& between) __attribute__((always_inline)) {
     if (fast && begun && key0 + 32 <= all_see && !bad) block(NO, sK, sV, key0, 0, between);
-    else if (key0 < some_see) block(YES, sK, sV, key0, bad, between);
+    else if (key0 < some_see && bad != NOTHING) block(YES, sK, sV, key0, bad, between);
     else between();
   };
   auto nothing = []() __attribute__((always_inline)) {};
@@ -691,7 +692,7 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
             for (int i = 0; i < 4; ++i)
               bad |= (unsigned)table[min((key0 + 8 * i) >> a.shift, last_entry)] < (unsigned)a.n_pages ? 0u : 1u << i;
           }
-          if (key0 < some_see) block(YES, lds + k_at(t) + kb * 32 * ROWB, lds + v_at(t) + kb * 32 * ROWB, key0, bad, nothing);
+          if (key0 < some_see && bad != NOTHING) block(YES, lds + k_at(t) + kb * 32 * ROWB, lds + v_at(t) + kb * 32 * ROWB, key0, bad, nothing);
         }
       }
       __syncthreads();
@@ -699,7 +700,6 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
       ++t;
       if ((t & 1) || t + 1 >= hot_end) continue;
       if (work) {
-        begun = true;  // (the references are those there are from here on)
         Piece kf[KS];
         f32x16 s0 = logits(lds), s1;
 #pragma unroll
