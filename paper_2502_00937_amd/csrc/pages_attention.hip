@@ -496,8 +496,9 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
   };
 
   // Weights are exp2(x - m) with the maximum m of the row's first block for all of its keys, which serves any row whose sum of
-  // weights stays between 2^-100 and 2^100 (bf16 and fp32 have the same exponents, so nothing is lost); a wave with another
-  // row goes over its keys again with a running maximum (`fast` is false then).
+  // weights stays between 2^-100 and 2^100 (bf16 and fp32 have the same exponents, so no weight is lost) and whose weighted values stay
+  // below 2^100, so that joining them stays finite too; a wave with another row goes over its keys again with a running maximum
+  // (`fast` is false then): no weight is above one.
   bool fast = true, begun = false;
   float neg_m = 0.f;
   auto logits = [&](const unsigned char* sK) __attribute__((always_inline)) {
@@ -783,11 +784,17 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
     finish();
   };
 
-  // a row that sees keys of this part and whose sum is out of range, or whose weights were measured against no maximum at all: its logits
+  // a row that sees keys of this part and whose sums are out of range, or whose weights were measured against no maximum at all: its logits
   // in the first block were minus infinity.  (So that wherever sums are joined, one that is not zero has a reference.)
   auto out_of_range = [&]() __attribute__((always_inline)) {
     const bool sees_some = first * item_keys < seen;
-    return __builtin_amdgcn_ballot_w64(sees_some && (m == -INFINITY || !(l >= 0x1p-100f && l <= 0x1p100f))) != 0;
+    f32x4 size = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) size[v & 3] += fabsf(o[b][v]);
+    const bool in_range = l >= 0x1p-100f && l <= 0x1p100f && (size[0] + size[1]) + (size[2] + size[3]) < 0x1p100f;
+    return __builtin_amdgcn_ballot_w64(sees_some && (m == -INFINITY || !in_range)) != 0;
   };
   if constexpr (NARROW) {
     if (all == 0) {

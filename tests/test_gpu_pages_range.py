@@ -70,3 +70,41 @@ def test_pages_that_were_given_up(dtype, fresh):
     for r, gone in enumerate((16, 39, 79)):
         c["block_table"][r, :gone] = -1
     check_range(c, lens, True, 64 ** -0.5, f"{fresh} rows, first pages given up")
+
+
+LARGE = {
+    "several steps a wave": [(1, 512)] * 64,
+    "parts of one token's keys": [(1, 131072)],
+    "one row tile": [(200, 900)],
+    "parts of a row tile's keys": [(200, 5000)],
+    "many rows": [(700, 900), (3, 20)],
+    "many rows, parts": [(700, 6000)],
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("name", LARGE)
+@pytest.mark.parametrize("size,late", [(1e30, 40.0), (1e30, 0.0), (1e9, 66.0), (3e33, 0.0)])
+def test_visible_values_of_any_size(dtype, name, size, late):
+    """Finite values that softmax would average: no sum of weighted values on the way may pass the type's largest number only
+    because a row's first keys have logits of about 0 and a later one has 40.  (131072 values of 1e33 stay below it.)"""
+    import torch
+
+    lens = LARGE[name]
+    if size > 1e33 and max(k for _, k in lens) * 1.5 * size > 3.4e38:
+        size = 1e33
+    c = make_case(dtype, 8, 8, 64, 16, lens)
+    rng = np.random.default_rng(3)
+    logits = []
+    for new, keys in lens:
+        x = rng.uniform(-1, 1, keys)
+        x[(np.arange(keys) % 61 == 60) & (np.arange(keys) > 40)] = late
+        logits.append(x)
+    set_logits(c, lens, logits)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for r, (_, keys) in enumerate(lens):
+        at = torch.arange(keys, device="cuda")
+        v = (torch.rand(keys, 8, 64, device="cuda", generator=g) + 0.5) * torch.where(torch.rand(keys, 8, 64, device="cuda", generator=g) < 0.3, -size, size)
+        c["value_pages"][c["block_table"][r].long()[at // 16], :, at % 16] = v.to(c["q"].dtype)
+    for causal in (True, False):
+        check_range(c, lens, causal, 1.0, f"{name}, values of {size}")
