@@ -785,11 +785,11 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
     finish();
   };
 
-  // A row that sees keys of this part and whose sums are out of
+  // A row that sees keys of this wave's (NARROW: they begin at its own place in a step; pages may hide them all) and whose sums are out of
   // range, or whose weights were measured against no maximum at all: its logits in the first block were minus infinity.  (So
   // that wherever sums are joined, one that is not zero has a reference.)
   auto out_of_range = [&]() __attribute__((always_inline)) {
-    const bool sees_some = first * item_keys < seen;
+    const bool sees_some = begun && (NARROW ? step_key(first) : first * item_keys) < seen;
     auto some_row = [](bool it) __attribute__((always_inline)) { return __builtin_amdgcn_ballot_w64(it) != 0; };
     const bool sees_without = sees_some && !(m > -INFINITY);
     if (!some_row(sees_without || (sees_some && !(l >= 0x1p-100f && l <= 0x1p10f)))) return false;

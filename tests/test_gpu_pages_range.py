@@ -108,3 +108,18 @@ def test_visible_values_of_any_size(dtype, name, size, late):
         c["value_pages"][c["block_table"][r].long()[at // 16], :, at % 16] = v.to(c["q"].dtype)
     for causal in (True, False):
         check_range(c, lens, causal, 1.0, f"{name}, values of {size}")
+
+
+@pytest.mark.parametrize("heads", [512])
+def test_a_row_that_sees_none_of_a_waves_keys(heads):
+    """32 tokens of 63 keys: the first one sees keys 0 to 31 and so none of the second wave's.  That sends no wave over its keys
+    again: without that token the others' bits are the same."""
+    import torch
+
+    import paper_2502_00937_amd as V
+
+    for seed in range(3):
+        c = make_case("bf16", heads, heads, 128, 16, [(32, 63)], seed=seed, spread=6.0)
+        got = V.attend_pages(**c)
+        rest = V.attend_pages(**dict(c, q=c["q"][1:], query_offsets=dev([0, 31])))
+        assert torch.equal(got[1:], rest)
