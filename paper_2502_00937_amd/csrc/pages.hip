@@ -215,7 +215,12 @@ __global__ __launch_bounds__(256) void plan_slots_kernel(const PlanArgs a) {
   }
   if (mine) a.slots[t] = slot;
   const int lost = __popcll(__builtin_amdgcn_ballot_w64(inside && slot < 0));
-  if (lost && (threadIdx.x & 63) == 0) atomicAdd(a.counts + 1, lost);  // (a sum of whole numbers: the order changes nothing)
+  if (lost && (threadIdx.x & 63) == 0) {
+    // A sum of whole numbers: the order changes nothing.  It stops at the largest one: of the waves that find it above, each brings it
+    // down behind its own addition, and all rows together are fewer than 2^30, so that it stays inside 32 bits meanwhile.
+    uint32_t* const count = (uint32_t*)a.counts + 1;
+    if (atomicAdd(count, (uint32_t)lost) + (uint32_t)lost > (uint32_t)INT32_MAX) atomicMin(count, (uint32_t)INT32_MAX);
+  }
 }
 
 // ---- append -------------------------------------------------------------------------------

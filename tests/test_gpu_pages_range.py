@@ -123,3 +123,26 @@ def test_a_row_that_sees_none_of_a_waves_keys(heads):
         got = V.attend_pages(**c)
         rest = V.attend_pages(**dict(c, q=c["q"][1:], query_offsets=dev([0, 31])))
         assert torch.equal(got[1:], rest)
+
+
+@pytest.mark.parametrize("form", ["more requests than a workgroup's", "in place"])
+def test_plan_tokens_without_a_slot_past_31_bits(form):
+    """More tokens past n_rows than 31 bits hold, and none of the rows gets a slot: the count stops at 2^31 - 1."""
+    import paper_2502_00937_amd as V
+
+    n, rows = (1025, 4096) if form != "in place" else (600, 5000)
+    cached, new, table = [0] * n, [2 ** 22] * n, np.full((n, 3), -1)
+    lens, taken, t = dev(cached), dev([0, 0]), dev(table)
+    out = None if form != "in place" else V.PagePlan(dev([7] * rows), dev([0] * (n + 1)), lens, dev([0] * (n + 1)), taken)
+    plan = V.plan_pages(lens, dev(new), t, dev([-1, -1]), taken, 50, 16, rows, out=out)
+    assert plan.counts.tolist() == [2, 2 ** 31 - 1]
+    assert plan.slots.tolist() == [-1] * rows
+    assert plan.query_offsets.tolist() == [0] + [rows] * n
+    # as many as 31 bits hold, and one fewer
+    for less in (0, 1, 5):
+        new = [2 ** 30, 2 ** 30 - 1 - less] + [0] * (n - 2)
+        lens, taken, t = dev(cached), dev([0, 0]), dev(table)
+        if out is not None:
+            out = V.PagePlan(dev([7] * rows), dev([0] * (n + 1)), lens, dev([0] * (n + 1)), taken)
+        plan = V.plan_pages(lens, dev(new), t, dev([-1, -1]), taken, 50, 16, rows, out=out)
+        assert plan.counts.tolist() == [2, 2 ** 31 - 1 - less]
