@@ -333,11 +333,11 @@ vit_status_t vit_preprocess_tiles(const uint8_t* image, int32_t height, int32_t 
  * pages whose number lies outside 0 ... n_pages - 1) has no effect, infinities and NaN among it.  Lengths are 0 to 2^31 - 256 (a
  * negative one counts as 0, a larger one as that).  Rows behind the last request's are left as they
  * are.  max_new: no request has more rows (of one that has, those past max_new are left as they are).  Logits, softmax and
- * sums are fp32: finite values give a finite result as long as a row's keys, or 2^20, times the
- * largest value it sees stay below 2^128.
- * (Of more than 2^24 keys of like weight that one part holds, the last lose their share of it.)  In bf16 the weights are rounded to bf16 ahead of the second product.  The keys' axis is divided
- * by what the batch leaves of the device and its parts are joined in order, so the last bits of a row depend on the batch, never on
- * timing.  The lengths and the table must not change while the call is at work.
+ * sums are fp32: finite values give a finite result as long as a row's keys, or 2^20, times the largest value it sees stay below
+ * 2^128.  A sum runs over 2^16 keys at the most in fp32 and 2^18 in bf16; longer ones are joined from such, so that rounding stays
+ * below 2^-9 of the row's weighted values however many there are.  In bf16 the weights are rounded to bf16 ahead of the second
+ * product.  The keys' axis is divided by what the batch leaves of the device and its parts are joined in order, so the last bits of
+ * a row depend on the batch, never on timing.  The lengths and the table must not change while the call is at work.
  * n_rows * q_heads is below 2^31, n_requests * kv_heads plus the row tiles (of 128 rows of a request and head of keys) below 2^24 - 512.
  * head_dim is a multiple of 8, at most 128; q_heads a multiple of kv_heads; scale finite; pointers and rows multiples of 16 bytes.
  * vit_pages_attend_query: bytes of workspace that the call needs (pointers in the struct are not looked at); the workspace is

@@ -41,7 +41,8 @@ struct PagedArgs {
   const int32_t *table, *starts, *kv;
   // workspace, all nullptr if no request's keys can be divided.  What the join needs to know (NARROW, int64: the steps of a head
   // of keys, then the steps before each request; WIDE, int32: whether anything was divided, nothing, then every request's
-  // first part and parts); reference maximum and sum of every part's rows; their unnormalised values
+  // first part and parts); reference maximum and sum of every part's rows; their unnormalised values (and,
+  // behind max_parts of them, those that a workgroup of WIDE has so far of more keys than a sum takes)
   int32_t* head;
   float *stats, *parts;
   int64_t max_parts;
@@ -61,6 +62,11 @@ constexpr int MOST_KEYS = INT32_MAX - 255;  // of a request: a few steps behind 
 // WIDE: a part of few steps is mostly its own start and its sums' way through memory, so it has 16 steps at the least (512 tokens 29.5
 // us, 30.6 without the limit; 16 requests of 100 tokens 25.6 and 29; with 32 steps 256 tokens over 8000 keys take 67 us for 58).
 constexpr int LEAST_STEPS = 16;
+// Keys that one sum runs over, in fp32 and in bf16.  A sum of n terms of like size is off by n / 2 roundings of it at the most and stops at 2^24
+// terms: 600 rows over 2^31 keys, all values one, came out as 0.8.  So longer runs are cut into sums that are joined as parts are:
+// off by 2^-9 at the most, of itself (bf16's instruction adds several products before it rounds).
+template <typename T>
+constexpr int LONG_SUM = sizeof(T) == 4 ? 1 << 16 : 1 << 18;
 
 template <typename T, int DB_, bool NARROW>
 struct Shape {
@@ -82,6 +88,7 @@ struct Shape {
   static constexpr int PAIRS = NARROW && ES == 4 ? 2 : 1;
   static constexpr int ITEM_ROWS = NARROW ? 32 * PAIRS : 128;
   static constexpr int ITEM_KEYS = NARROW ? 128 : 64;        // keys of a step of the whole workgroup, if its waves all have their own
+  static constexpr int LONG = LONG_SUM<T> / (NARROW ? 32 : 64);  // steps that a wave adds up at a time
 };
 
 // ---- a workgroup's place ------------------------------------------------------------------
@@ -91,6 +98,7 @@ struct Item {
   int first, last;             // NARROW: which steps of its keys
   int part;                    // where its results go if they are a part (WIDE: the request's first part), else -1
   int start, fresh, kv, rows;  // the request's first row, rows, keys; rows of (request, head of keys)
+  int stretch;                 // which Shape::LONG of its steps
 };
 
 struct Request {
@@ -176,7 +184,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs& a, int at, Item& foun
       if (i >= 0 && i < n) {
         // a request's longest row tile (the last one, if causal) first
         found = Item{base + tid, q.tiles - 1 - (int)i / splits, (int)i % splits, splits, 0, 0, splits > 1 ? (int)(before >> 32) : -1,
-                     q.start, q.fresh, q.kv, rows};
+                     q.start, q.fresh, q.kv, rows, 0};
       }
       __syncthreads();
       if (found.r >= 0) return true;
@@ -193,7 +201,7 @@ __device__ __forceinline__ Item uniform(const Item& i) {  // the same for all th
   return Item{__builtin_amdgcn_readfirstlane(i.r), __builtin_amdgcn_readfirstlane(i.tile), __builtin_amdgcn_readfirstlane(i.split),
               __builtin_amdgcn_readfirstlane(i.splits), __builtin_amdgcn_readfirstlane(i.first), __builtin_amdgcn_readfirstlane(i.last),
               __builtin_amdgcn_readfirstlane(i.part), __builtin_amdgcn_readfirstlane(i.start), __builtin_amdgcn_readfirstlane(i.fresh),
-              __builtin_amdgcn_readfirstlane(i.kv), __builtin_amdgcn_readfirstlane(i.rows)};
+              __builtin_amdgcn_readfirstlane(i.kv), __builtin_amdgcn_readfirstlane(i.rows), __builtin_amdgcn_readfirstlane(i.stretch)};
 }
 
 // NARROW: the steps of all heads, requests and row tiles, one after the other, are dealt out evenly: workgroup b of 2^slots takes
@@ -252,16 +260,29 @@ __device__ __forceinline__ uint32_t no_numbers(uint32_t w) {
   else return ((w & 0x7F800000u) + 0x00800000u) & 0x80000000u;
 }
 
-// One item: a row tile of a request and a head of keys, and the steps of its keys that are this workgroup's.
+// One item: a row tile of a request and a head of keys, and the steps of its keys that are this workgroup's (Shape::LONG of them: true if there
+// are more behind those).
 template <typename T, int DB, bool NARROW>
-__device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, const int kv_head, unsigned char* const lds) {
+__device__ __forceinline__ bool work_on(const PagedArgs& args, const Item& found, const int kv_head, unsigned char* const lds) {
   using Sh = Shape<T, DB, NARROW>;
   constexpr bool BF16 = sizeof(T) == 2;
   constexpr int KS = Sh::KS, ROWB = Sh::ROWB;
   typedef typename std::conditional<BF16, bf16x8, f32x4>::type Piece;
 
+  // WIDE: nothing is kept from one stretch to the next, as it would be registers that are not there: not what follows from the thread's
+  // number, nor the arguments
+  PagedArgs again;
+  if (!NARROW) {
+    typedef const __attribute__((address_space(4))) PagedArgs* ConstantArgs;
+    ConstantArgs from = (ConstantArgs)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(from));
+    __builtin_memcpy(&again, (const PagedArgs*)from, sizeof again);
+  }
+  const PagedArgs& a = NARROW ? args : again;
   const Item it = uniform(found);
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int tid = threadIdx.x;
+  if (!NARROW) asm volatile("" : "+v"(tid));
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 31, g = lane >> 5;
   if (!NARROW && a.head && tid == 0 && kv_head == 0 && it.tile == 0 && it.split == 0) {
     a.head[2 + 2 * it.r] = it.part;
@@ -294,6 +315,9 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
     first = __builtin_amdgcn_readfirstlane(it.split * even + min(it.split, more));
     last = __builtin_amdgcn_readfirstlane(first + even + (it.split < more ? 1 : 0));
   }
+  first += it.stretch * Sh::LONG;  // (at most `last`: the stretch before had steps left)
+  const bool unfinished = last - first > Sh::LONG;
+  if (unfinished) last = first + Sh::LONG;
 
   Piece qf[KS];
   int pieces = a.dh * Sh::ES / 16;  // of a head's row
@@ -379,7 +403,9 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
 
   // pieces that no load writes are zeros: they meet zeros of the queries
   if (!full) {
-    for (int i = tid; i < Sh::LDS / 16; i += THREADS) ((u32x4*)lds)[i] = u32x4{0u, 0u, 0u, 0u};
+    u32x4 zeros = {0u, 0u, 0u, 0u};
+    asm volatile("" : "+v"(zeros));  // (not kept either)
+    for (int i = tid; i < Sh::LDS / 16; i += THREADS) ((u32x4*)lds)[i] = zeros;
     __syncthreads();
   }
 
@@ -833,83 +859,136 @@ __device__ __forceinline__ void work_on(const PagedArgs& a, const Item& found, c
   // ---- results: a lane owns a row; registers 4 j .. 4 j + 3 of block b are its columns 32 b + 8 j + 4 g .. + 3
   const Item in = uniform(found);  // (read again: kept through the loops, it would be registers that they have not got)
   const int64_t part = NARROW ? in.part : in.part >= 0 ? ((int64_t)in.part + (int64_t)in.tile * in.splits + in.split) * a.kv_heads + kv_head : -1;
-  if (part >= a.max_parts) return;  // (only if the offsets are none: requests that overlap)
-  auto store = [&](int col, f32x4 v, int64_t at) __attribute__((always_inline)) {  // four columns of the row at element `at` of out
-    if constexpr (BF16) *(u32x2*)((bf16_t*)a.out + at + col) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-    else *(f32x4*)((float*)a.out + at + col) = v;
-  };
-  if constexpr (!NARROW) {
-    int own_row = row0 + lq;
-    asm volatile("" : "+v"(own_row));  // (worked out here, not ahead of the loops)
-    if (!active || own_row >= in.rows) return;
-    const int token = own_row / a.group, head = kv_head * a.group + (own_row - token * a.group);
-    const int64_t at = (int64_t)(in.start + token) * a.out_stride + (int64_t)head * a.dh;
-    const float inv = part >= 0 ? 1.f : l == 0.f ? 0.f : 1.f / l;
-    float* const po = a.parts + (part * a.part_rows + wave * 32 + lq) * (DB * 32);
-    if (part >= 0 && g == 0) {
-      a.stats[(part * a.part_rows + wave * 32 + lq) * 2] = m;
-      a.stats[(part * a.part_rows + wave * 32 + lq) * 2 + 1] = l;
-    }
+  if (part < a.max_parts) {  // (always, unless the offsets are none: requests that overlap)
+    // Stretches are added up in the part's place, or in one of the workgroup's own: NARROW's second part, which is written last if at all
+    const bool begun_before = in.stretch > 0, to_place = part >= 0 || unfinished;
+    const int64_t place = part >= 0 ? part : NARROW ? 2 * (int64_t)blockIdx.x + 1 : a.max_parts + blockIdx.x;
+    // sums so far (their reference and sum of weights) and this stretch's -> the factors of either, their common reference and sum
+    struct Both { float before, now, top, sum; };
+    auto both = [](float top0, float sum0, float top, float sum) __attribute__((always_inline)) {
+      const float up = fmaxf(sum0 == 0.f ? -INFINITY : top0, sum == 0.f ? -INFINITY : top);
+      const float f0 = sum0 == 0.f ? 0.f : __builtin_amdgcn_exp2f(top0 - up), f = sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(top - up);
+      return Both{f0, f, up, fmaf(sum0, f0, sum * f)};
+    };
+    auto store = [&](int col, f32x4 v, int64_t at) __attribute__((always_inline)) {  // four columns of the row at element `at` of out
+      if constexpr (BF16) *(u32x2*)((bf16_t*)a.out + at + col) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+      else *(f32x4*)((float*)a.out + at + col) = v;
+    };
+    if constexpr (!NARROW) {
+      int thread = threadIdx.x;
+      asm volatile("" : "+v"(thread));  // (what follows is worked out here, not ahead of the loops)
+      const int lq = thread & 31, g = thread >> 5 & 1, wave = thread >> 6, own_row = in.tile * Sh::ITEM_ROWS + wave * 32 + lq;
+      if (own_row < in.rows) {
+        const int token = own_row / a.group, head = kv_head * a.group + (own_row - token * a.group);
+        const int64_t at = (int64_t)(in.start + token) * a.out_stride + (int64_t)head * a.dh;
+        float* const stats = a.stats + (place * a.part_rows + wave * 32 + lq) * 2;
+        float* const po = a.parts + (place * a.part_rows + wave * 32 + lq) * (DB * 32);
+        if (begun_before) {
+          const Both x = both(stats[0], stats[1], m, l);
+          m = x.top;
+          l = x.sum;
 #pragma unroll
-    for (int b = 0; b < DB; ++b)
+          for (int b = 0; b < DB; ++b)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int col = 32 * b + 8 * j + 4 * g;
-        const f32x4 v = {o[b][4 * j] * inv, o[b][4 * j + 1] * inv, o[b][4 * j + 2] * inv, o[b][4 * j + 3] * inv};
-        if (part >= 0) *(f32x4*)(po + col) = v;
-        else if (col < a.dh) store(col, v, at);
-      }
-  } else {
-    // the four waves' sums are joined: each brought to the largest of their maxima
-    __syncthreads();
-    float* const ms = (float*)lds;              // [4][32] maxima, [4][32] sums
-    float* const so = (float*)(lds + 1024);     // [4][32][32 DB + 4]: rows a bank apart
-    constexpr int LD = DB * 32 + 4;
-    const int rows = min(32, in.rows - row0), tile_row = in.tile * Sh::ITEM_ROWS, tile_rows = min(Sh::ITEM_ROWS, in.rows - tile_row);
-    if (g == 0) {
-      ms[wave * 32 + lq] = m;
-      ms[128 + wave * 32 + lq] = l;
-    }
-    if (lq < rows) {
+            for (int j = 0; j < 4; ++j) {
+              const f32x4 v = *(const f32x4*)(po + 32 * b + 8 * j + 4 * g);
 #pragma unroll
-      for (int b = 0; b < DB; ++b)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          *(f32x4*)(so + (wave * 32 + lq) * LD + 32 * b + 8 * j + 4 * g) = f32x4{o[b][4 * j], o[b][4 * j + 1], o[b][4 * j + 2], o[b][4 * j + 3]};
-    }
-    __syncthreads();
-    constexpr int QUADS = DB * 8;
-    for (int i = tid; i < tile_rows * QUADS; i += THREADS) {
-      const int r = i / QUADS, col = (i - r * QUADS) * 4;
-      const int at = pairs ? r + (r & 32) : r, waves = pairs ? 2 : 4;  // the first wave that has the row, its numbers' place; how many have
-      float top = ms[at];
-#pragma unroll
-      for (int w = 1; w < 4; ++w)
-        if (w < waves) top = fmaxf(top, ms[w * 32 + at]);
-      const float ref = top == -INFINITY ? 0.f : top;
-      f32x4 v = {0.f, 0.f, 0.f, 0.f};
-      float sum = 0.f;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        if (w >= waves || ms[128 + w * 32 + at] == 0.f) continue;  // (it saw nothing)
-        const float mw = ms[w * 32 + at], f = __builtin_amdgcn_exp2f((mw == -INFINITY ? 0.f : mw) - ref);
-        const f32x4 x = *(const f32x4*)(so + (w * 32 + at) * LD + col);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = fmaf(x[e], f, v[e]);
-        sum = fmaf(ms[128 + w * 32 + at], f, sum);
-      }
-      const int tok = (tile_row + r) / a.group, hd = kv_head * a.group + (tile_row + r - tok * a.group);
-      if (part >= 0) {
-        *(f32x4*)(a.parts + (part * a.part_rows + r) * (DB * 32) + col) = v;
-        if (col == 0) {
-          a.stats[(part * a.part_rows + r) * 2] = top;
-          a.stats[(part * a.part_rows + r) * 2 + 1] = sum;
+              for (int e = 0; e < 4; ++e) o[b][4 * j + e] = fmaf(v[e], x.before, o[b][4 * j + e] * x.now);
+            }
         }
-      } else if (col < a.dh) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        store(col, f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv}, (int64_t)(in.start + tok) * a.out_stride + (int64_t)hd * a.dh);
+        const float inv = to_place ? 1.f : l == 0.f ? 0.f : 1.f / l;
+        if (to_place && g == 0) {
+          stats[0] = m;
+          stats[1] = l;
+        }
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int col = 32 * b + 8 * j + 4 * g;
+            const f32x4 v = {o[b][4 * j] * inv, o[b][4 * j + 1] * inv, o[b][4 * j + 2] * inv, o[b][4 * j + 3] * inv};
+            if (to_place) *(f32x4*)(po + col) = v;
+            else if (col < a.dh) store(col, v, at);
+          }
+      }
+    } else {
+      // the four waves' sums are joined: each brought to the largest of their maxima
+      __syncthreads();
+      float* const ms = (float*)lds;              // [4][32] maxima, [4][32] sums
+      float* const so = (float*)(lds + 1024);     // [4][32][32 DB + 4]: rows a bank apart
+      constexpr int LD = DB * 32 + 4;
+      const int rows = min(32, in.rows - row0), tile_row = in.tile * Sh::ITEM_ROWS, tile_rows = min(Sh::ITEM_ROWS, in.rows - tile_row);
+      if (g == 0) {
+        ms[wave * 32 + lq] = m;
+        ms[128 + wave * 32 + lq] = l;
+      }
+      if (lq < rows) {
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            *(f32x4*)(so + (wave * 32 + lq) * LD + 32 * b + 8 * j + 4 * g) = f32x4{o[b][4 * j], o[b][4 * j + 1], o[b][4 * j + 2], o[b][4 * j + 3]};
+      }
+      __shared__ float so_far[Sh::ITEM_ROWS][2];  // references and sums of the stretches before
+      if (begun_before && tid < tile_rows) {
+        so_far[tid][0] = a.stats[(place * a.part_rows + tid) * 2];
+        so_far[tid][1] = a.stats[(place * a.part_rows + tid) * 2 + 1];
+      }
+      __syncthreads();
+      constexpr int QUADS = DB * 8;
+      for (int i = tid; i < tile_rows * QUADS; i += THREADS) {
+        const int r = i / QUADS, col = (i - r * QUADS) * 4;
+        const int at = pairs ? r + (r & 32) : r, waves = pairs ? 2 : 4;  // the first wave that has the row, its numbers' place; how many have
+        float top = ms[at];
+#pragma unroll
+        for (int w = 1; w < 4; ++w)
+          if (w < waves) top = fmaxf(top, ms[w * 32 + at]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          if (w >= waves || ms[128 + w * 32 + at] == 0.f) continue;  // (it saw nothing)
+          const float mw = ms[w * 32 + at], f = __builtin_amdgcn_exp2f((mw == -INFINITY ? 0.f : mw) - ref);
+          const f32x4 x = *(const f32x4*)(so + (w * 32 + at) * LD + col);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = fmaf(x[e], f, v[e]);
+          sum = fmaf(ms[128 + w * 32 + at], f, sum);
+        }
+        const int tok = (tile_row + r) / a.group, hd = kv_head * a.group + (tile_row + r - tok * a.group);
+        float* const po = a.parts + (place * a.part_rows + r) * (DB * 32) + col;
+        if (begun_before) {
+          const Both x = both(so_far[r][0], so_far[r][1], top, sum);
+          const f32x4 w = *(const f32x4*)po;
+          top = x.top;
+          sum = x.sum;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = fmaf(w[e], x.before, v[e] * x.now);
+        }
+        if (to_place) {
+          *(f32x4*)po = v;
+          if (col == 0) {
+            a.stats[(place * a.part_rows + r) * 2] = top;
+            a.stats[(place * a.part_rows + r) * 2 + 1] = sum;
+          }
+        } else if (col < a.dh) {
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          store(col, f32x4{v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv}, (int64_t)(in.start + tok) * a.out_stride + (int64_t)hd * a.dh);
+        }
       }
     }
+  }
+  return __builtin_amdgcn_readfirstlane(unfinished && part < a.max_parts);
+}
+
+// All of an item's steps.
+template <typename T, int DB, bool NARROW>
+__device__ __forceinline__ void work_on_all(const PagedArgs& a, Item& found, const int kv_head, unsigned char* const lds) {
+#pragma unroll 1
+  while (work_on<T, DB, NARROW>(a, found, kv_head, lds)) {
+    __syncthreads();
+    if (threadIdx.x == 0) ++found.stretch;
+    __syncthreads();
   }
 }
 
@@ -920,7 +999,7 @@ __global__ __launch_bounds__(THREADS, (NARROW || sizeof(T) == 4) && DB > 2 ? 1 :
   __shared__ Item found;
   if constexpr (!NARROW) {
     if (!find_item<Sh>(a, blockIdx.x / a.kv_heads, found)) return;
-    work_on<T, DB, NARROW>(a, found, blockIdx.x % a.kv_heads, lds);
+    work_on_all<T, DB, NARROW>(a, found, blockIdx.x % a.kv_heads, lds);
   } else {
     __shared__ int64_t sums[4], ahead[THREADS + 1];  // steps before each of the first requests, of a head of keys
     __shared__ Stretch stretch;
@@ -994,10 +1073,10 @@ __global__ __launch_bounds__(THREADS, (NARROW || sizeof(T) == 4) && DB > 2 ? 1 :
         if (tid == 0) {
           // a workgroup leaves a part of its first item and one of its last at the most
           const int part = first == 0 && last == end ? -1 : 2 * (int)blockIdx.x + (done == from ? 0 : 1);
-          found = Item{r, tile, 0, 1, first, last, part, q.start, q.fresh, q.kv, min(q.fresh, a.max_new) * a.group};
+          found = Item{r, tile, 0, 1, first, last, part, q.start, q.fresh, q.kv, min(q.fresh, a.max_new) * a.group, 0};
         }
         __syncthreads();
-        work_on<T, DB, NARROW>(a, found, kv_head, lds);
+        work_on_all<T, DB, NARROW>(a, found, kv_head, lds);
         __syncthreads();  // before LDS is used again
         done += last - first;
         at += last - first;
@@ -1123,7 +1202,7 @@ struct Layout {
   bool narrow;
   bool divide;
   int slots, part_rows, width;   // see PagedArgs; columns of a part's rows
-  int64_t grid, parts;
+  int64_t grid, parts, places;
   size_t head_bytes, stats_bytes, bytes;
 };
 
@@ -1149,11 +1228,14 @@ Layout lay_out(const vit_pages_attend_t* p) {
   y.grid = y.narrow ? y.slots : tiles + (y.divide ? y.slots : 0);
   // NARROW: two a workgroup.  WIDE: divided requests have more than one share each, so at most twice as many parts as shares.
   y.parts = !y.divide ? 0 : 2 * y.slots + (y.narrow ? 0 : p->kv_heads);
+  // WIDE: where the table has room for more keys than a sum takes, each workgroup has a place for them (64 KiB at 128 columns)
+  const bool longer = (int64_t)p->table_width * p->page_size > (p->dtype == VIT_DTYPE_FP32 ? LONG_SUM<float> : LONG_SUM<bf16_t>);
+  y.places = y.parts + (!y.narrow && longer ? y.grid : 0);
   if (y.divide) {
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     y.head_bytes = up(((size_t)p->n_requests + 1) * sizeof(int64_t));
-    y.stats_bytes = up((size_t)y.parts * y.part_rows * 2 * sizeof(float));
-    y.bytes = y.head_bytes + y.stats_bytes + (size_t)y.parts * y.part_rows * y.width * sizeof(float);
+    y.stats_bytes = up((size_t)y.places * y.part_rows * 2 * sizeof(float));
+    y.bytes = y.head_bytes + y.stats_bytes + (size_t)y.places * y.part_rows * y.width * sizeof(float);
   }
   return y;
 }

@@ -146,3 +146,83 @@ def test_plan_tokens_without_a_slot_past_31_bits(form):
             out = V.PagePlan(dev([7] * rows), dev([0] * (n + 1)), lens, dev([0] * (n + 1)), taken)
         plan = V.plan_pages(lens, dev(new), t, dev([-1, -1]), taken, 50, 16, rows, out=out)
         assert plan.counts.tolist() == [2, 2 ** 31 - 1 - less]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads,fresh", [(1, 600), (32, 1)])
+@pytest.mark.parametrize("value", [1.0, 83 / 64])
+def test_averages_over_as_many_keys_as_a_length_holds(dtype, heads, fresh, value):
+    """2^31 - 256 equal keys, all values the same: that value.  Sums are cut where rounding would pile up.  A sum of n equal terms is off
+    by n / 2 half steps of it at the most: 2^16 / 2 * 2^-24 = 2^-9 in fp32, and with four terms or more to a rounding of 2^18 / 4 in bf16
+    2^-9 too.  Joining 2^31 / 512 / 2^16 = 64 to 640 such sums and 512 parts takes three roundings of 2^-24 each: below 2^-12.
+    Then the output's half step."""
+    import torch
+
+    import paper_2502_00937_amd as V
+
+    say(f"case averages over 2^31 - 256 keys: {dtype}, {heads} heads, {fresh} rows, values {value}")
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    keys, values = (torch.full((2, heads, 4096, 8), x, dtype=t, device="cuda") for x in (0.0, value))
+    values[0] = float("nan")  # (a page that the table does not name)
+    q = torch.randn(fresh, heads, 8, device="cuda").to(t)
+    table = torch.ones(1, 1 << 19, dtype=torch.int32, device="cuda")
+    got = V.attend_pages(q, keys, values, table, dev([0, fresh]), dev([2 ** 31 - 1]), fresh)
+    worst = float((got.double() / value - 1).abs().max())
+    say(f"    off by {worst:.2e}")
+    assert worst <= 2 ** -9 + 2 ** -12 + torch.finfo(t).eps / 2
+
+
+@pytest.mark.parametrize("dtype,heads,fresh,keys,page", [
+    # a row tile that is whole, and parts of one, with more keys than a sum takes; then the same where waves have keys of their own
+    ("fp32", 512, 600, 150_000, 16), ("fp32", 2, 600, 50_000_000, 4096), ("fp32", 512, 1, 600_000, 16), ("fp32", 1, 2, 400_000_000, 4096),
+    ("fp32", 512, 40, 300_000, 16), ("fp32", 3, 40, 200_000_000, 4096),
+    ("bf16", 512, 40, 600_000, 16), ("bf16", 2, 600, 40_000_000, 4096), ("bf16", 512, 1, 2_500_000, 64), ("bf16", 1, 2, 1_200_000_000, 4096),
+])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attend_more_keys_than_a_sum_takes(dtype, heads, fresh, keys, page, causal):
+    """Few different tokens, again and again in the order of a table that names their pages: softmax over the tokens, each counted as often
+    as a row sees it.  The tokens of the beginning, the middle and the end have values around 1, 0 and -1, so that a stretch that is
+    lost or counted twice shows.  Tolerances as in `plain_attend`, with sums of 2^16 (fp32: n / 2 roundings of 2^-24, twice: 2^-8) or 2^18
+    terms (bf16: four terms or more to a rounding, 2^-8 too), and three roundings of each joined sum, below 2^-12."""
+    import torch
+
+    import paper_2502_00937_amd as V
+
+    say(f"case many keys: {dtype}, {heads} heads, {fresh} rows of {keys} keys, pages of {page}, causal {causal}")
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(keys % 1000)
+    per_third = 2 if page > 1000 else 12
+    pages, dim = 3 * per_third + 1, 8
+    pools = torch.randn(2, pages, heads, page, dim, device="cuda", generator=g)
+    pools[1] *= 0.1
+    for third in range(3):
+        pools[1, third * per_third:(third + 1) * per_third] += 1 - third
+    pools = pools.to(t)
+    pools[:, -1] = float("nan")
+    entries = -(-keys // page)
+    third = torch.arange(entries, device="cuda") * 3 // entries
+    table = (third * per_third + torch.randint(0, per_third, (entries,), device="cuda", generator=g)).to(torch.int32)
+    q = torch.randn(fresh, heads, dim, device="cuda", generator=g).to(t)
+    got = V.attend_pages(q, pools[0], pools[1], table[None], dev([0, fresh]), dev([keys]), fresh, causal=causal)
+    # how often each token lies in the keys that a row sees: all of them, less the last ones one by one
+    tokens = (pages - 1) * page
+    counts = torch.zeros(tokens, dtype=torch.float64, device="cuda")
+    whole = torch.bincount(table[:-1].long(), minlength=pages - 1).double()
+    counts += whole.repeat_interleave(page)
+    counts[int(table[-1]) * page:int(table[-1]) * page + keys - (entries - 1) * page] += 1
+    at = torch.arange(keys - fresh, keys, device="cuda")
+    last = torch.zeros(fresh, tokens, dtype=torch.float64, device="cuda")
+    last[torch.arange(fresh, device="cuda"), table[at // page].long() * page + at % page] = 1
+    seen = counts - last.flip(0).cumsum(0).flip(0) + last if causal else counts.expand(fresh, -1)  # (a row's own key and those before)
+    assert float(seen[-1].sum()) == keys and float(seen[0].sum()) == (keys - fresh + 1 if causal else keys)
+    for h in range(0, heads, max(1, heads // 8)):
+        k, v = (p[:-1, h].reshape(tokens, dim).double() for p in pools)
+        x = q[:, h].double()
+        logits = x @ k.T.contiguous() * dim ** -0.5
+        w = seen * torch.exp(logits - logits.amax(1, keepdim=True))
+        w /= w.sum(1, keepdim=True)
+        want, mass = w @ v, w @ v.abs()
+        size = (x.abs() @ k.abs().T.contiguous() * dim ** -0.5).amax(1, keepdim=True)
+        u = torch.finfo(t).eps / 2
+        off = 2 * (u if t == torch.bfloat16 else 0) + 2 * (dim + 8) * 2.0 ** -24 * size + 2.0 ** -8 + 2.0 ** -12
+        compare(got[:, h], want, off * mass + u * want.abs(), f"head {h}")
