@@ -339,7 +339,7 @@ vit_status_t vit_preprocess_tiles(const uint8_t* image, int32_t height, int32_t 
  * product.  The keys' axis is divided by what the batch leaves of the device and its parts are joined in order, so the last bits of
  * a row depend on the batch, never on timing.  The lengths and the table must not change while the call is at work.
  * n_rows * q_heads is below 2^31, n_requests * kv_heads plus the row tiles (of 128 rows of a request and head of keys) below 2^24 - 512.
- * head_dim is a multiple of 8, at most 128; q_heads a multiple of kv_heads; scale finite; pointers and rows multiples of 16 bytes.
+ * head_dim is a multiple of 8, at most 128; q_heads a multiple of kv_heads; scale finite, times log2(e) too; pointers and rows multiples of 16 bytes.
  * vit_pages_attend_query: bytes of workspace that the call needs (pointers in the struct are not looked at); the workspace is
  * 256-byte aligned, its contents undefined before and after, and no two calls at work at a time may share it.
  * Errors: VIT_EINVAL (NULL, sizes, alignment), VIT_ECAPACITY (workspace), VIT_EDEVICE; nothing was launched.

@@ -51,7 +51,7 @@ struct PagedArgs {
   int divide;
   int slots;     // logarithm of the workgroups that the device holds at a time, which they are divided for
   int part_rows; // rows of a part
-  float scale;   // >= 0, times log2(e)
+  float scale;   // > 0, times log2(e)
   int negative;  // the scale's sign, which goes to the queries
 };
 
@@ -1207,6 +1207,7 @@ struct Layout {
 };
 
 constexpr int UNITS = 256;  // compute units of the device
+constexpr float LOG2E = 1.44269504088896340736f;
 
 Layout lay_out(const vit_pages_attend_t* p) {
   Layout y{};
@@ -1273,7 +1274,7 @@ vit_status_t check_sizes(const vit_pages_attend_t* p, const char* name) {
     return set_error(VIT_EINVAL, "%s: q_heads must be a multiple of kv_heads, at most 1024", name);
   if (p->n_rows < 0 || p->n_rows >= 1 << 30 || p->n_requests < 0 || p->n_requests > 1 << 20 || p->max_new < 0 || p->table_width < 0)
     return set_error(VIT_EINVAL, "%s: sizes must not be negative, n_rows < 2^30, n_requests <= 2^20", name);
-  if (!std::isfinite(p->scale)) return set_error(VIT_EINVAL, "%s: scale must be finite", name);
+  if (!std::isfinite(p->scale * LOG2E)) return set_error(VIT_EINVAL, "%s: scale must be finite, times log2(e) too", name);
   // so that numbers of rows, row tiles and workgroups stay inside 31 bits
   if ((int64_t)p->n_rows * p->q_heads >= (int64_t)1 << 31 || (int64_t)p->n_requests * p->kv_heads >= 1 << 30)
     return set_error(VIT_EINVAL, "%s: n_rows * q_heads must be below 2^31, n_requests * kv_heads below 2^30", name);
@@ -1319,8 +1320,9 @@ extern "C" vit_status_t vit_pages_attend(const vit_pages_attend_t* p, void* stre
   a.rows = p->n_rows; a.R = p->n_requests; a.max_new = p->max_new; a.width = p->n_pages > 0 ? p->table_width : 0; a.n_pages = p->n_pages;
   a.shift = __builtin_ctz(p->page_size); a.heads = p->q_heads; a.kv_heads = p->kv_heads; a.group = p->q_heads / p->kv_heads;
   a.dh = p->head_dim; a.causal = p->causal != 0; a.divide = y.divide;  a.slots = __builtin_ctz(y.slots);  a.part_rows = y.part_rows; a.max_parts = y.parts;
-  // (a scale of zero: all logits equal, and what no row sees still minus infinity)
-  a.scale = std::max(std::fabs(p->scale) * 1.44269504088896340736f, 1e-35f); a.negative = p->scale < 0;
+  // (a scale of zero: the smallest number there is, so that what no row sees is still minus infinity; the largest product of queries and
+  // keys times it is 2^-21)
+  a.scale = std::max(std::fabs(p->scale) * LOG2E, 0x1p-149f); a.negative = p->scale < 0;
   const hipError_t e = p->dtype == VIT_DTYPE_FP32 ? launch<float>(a, y, (hipStream_t)stream) : launch<bf16_t>(a, y, (hipStream_t)stream);
   if (e != hipSuccess) return set_error(VIT_EDEVICE, "vit_pages_attend: launch: %s", hipGetErrorString(e));
   return VIT_OK;

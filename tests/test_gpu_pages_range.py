@@ -226,3 +226,17 @@ def test_attend_more_keys_than_a_sum_takes(dtype, heads, fresh, keys, page, caus
         u = torch.finfo(t).eps / 2
         off = 2 * (u if t == torch.bfloat16 else 0) + 2 * (dim + 8) * 2.0 ** -24 * size + 2.0 ** -8 + 2.0 ** -12
         compare(got[:, h], want, off * mass + u * want.abs(), f"head {h}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-36, -1e-37, 3e-39])
+@pytest.mark.parametrize("lens", [[(1, 700), (3, 90)], [(150, 700), (600, 650)]], ids=["tokens", "chunks"])
+def test_scales_of_zero_and_next_to_it(dtype, scale, lens):
+    """Products of queries and keys of up to 6e37: times 0 all logits are equal, times 1e-36 they are tens apart."""
+    import torch
+
+    c = make_case(dtype, 4, 2, 64, 16, lens)
+    c["q"] = (c["q"].float() * 1e17).to(c["q"].dtype)
+    kept = c["key_pages"].float().abs() < 100
+    c["key_pages"] = torch.where(kept, c["key_pages"].float() * 1e18, c["key_pages"].float()).to(c["q"].dtype)
+    check_range(c, lens, True, scale, f"scale {scale}")
