@@ -276,7 +276,7 @@ __device__ __forceinline__ bool work_on(const PagedArgs& args, const Item& found
     typedef const __attribute__((address_space(4))) PagedArgs* ConstantArgs;
     ConstantArgs from = (ConstantArgs)__builtin_amdgcn_kernarg_segment_ptr();
     asm volatile("" : "+s"(from));
-    __builtin_memcpy(&again, (const PagedArgs*)from, sizeof again);
+    __builtin_memcpy(&again, (const PagedArgs*)from, sizeof again);  // (the kernel's only argument)
   }
   const PagedArgs& a = NARROW ? args : again;
   const Item it = uniform(found);
@@ -981,17 +981,6 @@ __device__ __forceinline__ bool work_on(const PagedArgs& args, const Item& found
   return __builtin_amdgcn_readfirstlane(unfinished && part < a.max_parts);
 }
 
-// All of an item's steps.
-template <typename T, int DB, bool NARROW>
-__device__ __forceinline__ void work_on_all(const PagedArgs& a, Item& found, const int kv_head, unsigned char* const lds) {
-#pragma unroll 1
-  while (work_on<T, DB, NARROW>(a, found, kv_head, lds)) {
-    __syncthreads();
-    if (threadIdx.x == 0) ++found.stretch;
-    __syncthreads();
-  }
-}
-
 template <typename T, int DB, bool NARROW>
 __global__ __launch_bounds__(THREADS, (NARROW || sizeof(T) == 4) && DB > 2 ? 1 : 2) void paged_attention_kernel(const PagedArgs a) {
   using Sh = Shape<T, DB, NARROW>;
@@ -999,7 +988,12 @@ __global__ __launch_bounds__(THREADS, (NARROW || sizeof(T) == 4) && DB > 2 ? 1 :
   __shared__ Item found;
   if constexpr (!NARROW) {
     if (!find_item<Sh>(a, blockIdx.x / a.kv_heads, found)) return;
-    work_on_all<T, DB, NARROW>(a, found, blockIdx.x % a.kv_heads, lds);
+#pragma unroll 1
+    while (work_on<T, DB, NARROW>(a, found, blockIdx.x % a.kv_heads, lds)) {
+      __syncthreads();
+      if (threadIdx.x == 0) ++found.stretch;
+      __syncthreads();
+    }
   } else {
     __shared__ int64_t sums[4], ahead[THREADS + 1];  // steps before each of the first requests, of a head of keys
     __shared__ Stretch stretch;
@@ -1068,18 +1062,24 @@ __global__ __launch_bounds__(THREADS, (NARROW || sizeof(T) == 4) && DB > 2 ? 1 :
       int tile = min((int)quotient(at - below, its), tiles - 1), first = (int)(at - below - (int64_t)tile * its);
       if (tile < 0 || first >= (tile == tiles - 1 ? last_its : its)) return;  // (likewise)
 #pragma unroll 1
-      for (; tile < tiles && done < to; ++tile, first = 0) {
+      for (int stretch = 0; tile < tiles && done < to;) {
         const int end = tile == tiles - 1 ? last_its : its, last = (int)min((int64_t)end, first + (to - done));
         if (tid == 0) {
           // a workgroup leaves a part of its first item and one of its last at the most
           const int part = first == 0 && last == end ? -1 : 2 * (int)blockIdx.x + (done == from ? 0 : 1);
-          found = Item{r, tile, 0, 1, first, last, part, q.start, q.fresh, q.kv, min(q.fresh, a.max_new) * a.group, 0};
+          found = Item{r, tile, 0, 1, first, last, part, q.start, q.fresh, q.kv, min(q.fresh, a.max_new) * a.group, stretch};
         }
         __syncthreads();
-        work_on_all<T, DB, NARROW>(a, found, kv_head, lds);
+        const bool more = work_on<T, DB, NARROW>(a, found, kv_head, lds);
         __syncthreads();  // before LDS is used again
+        if (more) {
+          ++stretch;
+          continue;
+        }
         done += last - first;
         at += last - first;
+        ++tile;
+        first = stretch = 0;
       }
       below += (int64_t)(tiles - 1) * its + last_its;
       ++r;
