@@ -322,8 +322,8 @@ vit_status_t vit_preprocess_tiles(const uint8_t* image, int32_t height, int32_t 
  * Outputs overlap neither inputs nor each other, but for the two named.
  *
  * vit_pages_append: rows i of k and v (head h's values at i * stride + h * head_dim) to slots[i] of the pools.  Rows with a slot
- * outside 0 ... n_pages * page_size - 1 are passed over.  No slot may be given twice.  Pointers and rows are multiples of
- * 16 bytes.  The rows' values of k are below 64 GiB together.
+ * outside 0 ... n_pages * page_size - 1 are passed over.  No slot may be given twice, and k and v lie outside the pools.  Pointers
+ * and rows are multiples of 16 bytes.  The rows' values of k are below 64 GiB together.
  *
  * vit_pages_attend: rows query_offsets[r] ... query_offsets[r + 1] - 1 of q and out are request r's; row i's head h (at
  * i * stride + h * head_dim) attends to its request's kv_lens[r] keys of head h / (q_heads / kv_heads):
@@ -335,9 +335,10 @@ vit_status_t vit_preprocess_tiles(const uint8_t* image, int32_t height, int32_t 
  * are.  max_new: no request has more rows (of one that has, those past max_new are left as they are).  Logits, softmax and
  * sums are fp32: finite values give a finite result as long as a row's keys, or 2^20, times the largest value it sees stay below
  * 2^128.  A sum runs over 2^16 keys at the most in fp32 and 2^18 in bf16; longer ones are joined from such, so that rounding stays
- * below 2^-9 of the row's weighted values however many there are.  In bf16 the weights are rounded to bf16 ahead of the second
+ * below 2^-8 of the row's weighted values however many there are.  In bf16 the weights are rounded to bf16 ahead of the second
  * product.  The keys' axis is divided by what the batch leaves of the device and its parts are joined in order, so the last bits of
- * a row depend on the batch, never on timing.  The lengths and the table must not change while the call is at work.
+ * a row depend on the batch, never on timing.  The lengths and the table must not change while the call is at work; out and the workspace
+ * overlap nothing that it reads, nor each other.
  * n_rows * q_heads is below 2^31, n_requests * kv_heads plus the row tiles (of 128 rows of a request and head of keys) below 2^24 - 512.
  * head_dim is a multiple of 8, at most 128; q_heads a multiple of kv_heads; scale finite, times log2(e) too; pointers and rows multiples of 16 bytes.
  * vit_pages_attend_query: bytes of workspace that the call needs (pointers in the struct are not looked at); the workspace is

@@ -3,7 +3,9 @@
 A layer's cache is two pools `[n_pages, kv_heads, page_size, head_dim]`, bf16 or fp32, that the caller owns; a request's row of
 the block table names its pages in order.  `plan_pages` gives a step's new tokens their pages and slots (once a step, for
 all layers), `append_pages` writes their keys and values, `attend_pages` lets their queries attend to the cache.  Every call is
-queued on the current stream of the tensors' device, waits for nothing and may be captured into a graph.
+queued on the current stream of the tensors' device, waits for nothing and may be captured into a graph.  The calls are for serving:
+tensors that require a gradient are taken for their numbers alone, results carry no graph, and what is written (pools, tables,
+`out`) is written without autograd's knowledge.
 """
 from __future__ import annotations
 
