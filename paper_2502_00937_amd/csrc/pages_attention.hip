@@ -10,7 +10,7 @@
 // 32 x 32 x 2 ones.
 //
 // Two forms.  WIDE: 128 rows a workgroup, 32 a wave, which share tiles of 64 keys; bound by the matrix units at the device's power limit
-// (4096 rows of 128 columns over 32768 keys 1.12 PFLOP/s; the causal half of 8192 tokens 0.92 to 0.97, by the device).  NARROW, where requests have few
+// (4096 rows of 128 columns over 32768 keys 1.06 to 1.14 PFLOP/s, by the device; the causal half of 8192 tokens 0.91 to 0.97).  NARROW, where requests have few
 // rows: the waves share 32 rows and each has keys of its own, so that four times as many loads are on their way and no
 // barrier stands between them (fp32: of more than 32 rows two waves have 32 each and two pairs the same keys, whose second
 // reader finds them in a cache: images 101.7 -> 97.4 us, with 128 columns 405 -> 358); bound by HBM (64 single tokens over 2.09 GB of keys and values 5.76 TB/s).

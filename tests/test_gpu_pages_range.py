@@ -240,3 +240,39 @@ def test_scales_of_zero_and_next_to_it(dtype, scale, lens):
     kept = c["key_pages"].float().abs() < 100
     c["key_pages"] = torch.where(kept, c["key_pages"].float() * 1e18, c["key_pages"].float()).to(c["q"].dtype)
     check_range(c, lens, True, scale, f"scale {scale}")
+
+
+@pytest.mark.parametrize("heads,fresh,keys", [(512, 600, 150_000), (2, 600, 3_000_000), (512, 1, 600_000)])
+def test_more_keys_than_a_sum_takes_in_graphs_and_on_streams(heads, fresh, keys):
+    """Sums so far lie in the workspace: two calls at once on two streams, and two graphs replayed in turn with other work between, have
+    the eager call's bits."""
+    import torch
+
+    import paper_2502_00937_amd as V
+
+    g = torch.Generator(device="cuda").manual_seed(keys % 1000)
+    pools = torch.randn(2, 41, heads, 16, 8, device="cuda", generator=g)
+    table = torch.randint(0, 41, (1, -(-keys // 16)), device="cuda", generator=g).to(torch.int32)
+    queries = [torch.randn(fresh, heads, 8, device="cuda", generator=g) for _ in range(2)]
+    rest = (pools[0], pools[1], table, dev([0, fresh]), dev([keys]), fresh)
+    want = [V.attend_pages(q, *rest) for q in queries]
+    assert not torch.equal(*want)
+    got = [torch.empty_like(w) for w in want]
+    streams, graphs = [torch.cuda.Stream() for _ in want], [torch.cuda.CUDAGraph() for _ in want]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for s, q, o in zip(streams, queries, got):
+            with torch.cuda.stream(s):
+                V.attend_pages(q, *rest, out=o)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for o, w in zip(got, want))
+    for graph, q, o in zip(graphs, queries, got):
+        with torch.cuda.graph(graph):
+            V.attend_pages(q, *rest, out=o)
+    for _ in range(3):
+        for graph, o in zip(graphs, got):
+            o.fill_(float("nan"))
+            graph.replay()
+        torch.cuda.synchronize()
+        torch.ones(1000, device="cuda").sum().item()
+        assert all(torch.equal(o, w) for o, w in zip(got, want))
